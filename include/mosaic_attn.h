@@ -356,6 +356,75 @@ MB_API mb_status mb_gelu_gate(const void* h, const void* gate, int64_t row_strid
                               int inter, mb_dtype dt, void* act, void* stream);
 
 /*
+ * Rows and weights in 8 bits.  A value is an OCP e4m3 byte (4 bits of exponent, 3 of mantissa, largest 448, 0x7f / 0xff NaN, no
+ * infinity) times a scale 2^(b - 127), whose byte b (E8M0, 255 = NaN) serves
+ *   rows     128 values of a row: q [T, W], s [T, ceil(W / 128)], the last block of a row may be shorter;
+ *   weights  a 128 x 128 block: q [n_out, n_in], s [ceil(n_out / 128), ceil(n_in / 128)], blocks at the ends may be smaller.
+ * All four are contiguous.  Widths are multiples of 16 up to 2^20.  Powers of two round nothing: x = q 2^(b - 127) is exact in
+ * float and, where it is a normal number, in bfloat16 (the largest floats, over 248 * 2^120, round up to 2^128: infinite again
+ * as a float).
+ *   Storing a block takes the smallest scale 2^e, e >= -126, with every finite |x| <= 448 * 2^e, and rounds x / 2^e to the nearest
+ *   e4m3 value (ties to even).  Infinities and NaN are stored as NaN and have no part in the scale.  A block of zeros has b = 1.
+ * T_cap, meta_dev: rows [0, T), T = min(meta_dev[0], T_cap) or T_cap if meta_dev is NULL; the others are neither read nor
+ * written.  Limits: T_cap <= 2^30, row strides < 2^21 elements and a multiple of 16 bytes (MB_ERR_UNSUPPORTED, MB_ERR_INVALID_ARG).
+ *
+ * mb_fp8_quant         x [T_cap, W] of row stride x_row_stride (elements), dt -> q, s.
+ * mb_fp8_dequant       q, s -> x, rounded once to dt.
+ * mb_fp8_quant_weight  w [n_out, n_in] contiguous, dt -> q, s and, unless both are NULL, the same values transposed: qt [n_in,
+ *                      n_out], st [ceil(n_in / 128), ceil(n_out / 128)] (what the data gradient of a product reads).
+ */
+MB_API mb_status mb_fp8_quant(const void* x, int64_t x_row_stride, int T_cap, const int32_t* meta_dev, int W, mb_dtype dt,
+                              uint8_t* q, uint8_t* s, void* stream);
+MB_API mb_status mb_fp8_dequant(const uint8_t* q, const uint8_t* s, int T_cap, const int32_t* meta_dev, int W, mb_dtype dt,
+                                void* x, int64_t x_row_stride, void* stream);
+MB_API mb_status mb_fp8_quant_weight(const void* w, int n_out, int n_in, mb_dtype dt, uint8_t* q, uint8_t* s, uint8_t* qt,
+                                     uint8_t* st, void* stream);
+
+/*
+ * Linear layer on 8-bit rows:  y[t, n] = sum_k x[t, k] w[n, k], fp32 sums, rounded once to dt.
+ *   xq, xs   dev, rows [T_cap, n_in], read.      wq, ws   dev, weight [n_out, n_in], read.
+ *   y        dev, [T_cap, n_out] of row stride y_row_stride, written.
+ * The data gradient dx = dy W is the same call: rows dy [T_cap, n_out] with the transposed weight qt, st of mb_fp8_quant_weight.
+ * T_cap * n_out < 2^38.
+ */
+MB_API mb_status mb_linear_fp8_fwd(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, int T_cap,
+                                   const int32_t* meta_dev, int n_in, int n_out, mb_dtype dt, void* y, int64_t y_row_stride,
+                                   void* stream);
+
+/*
+ * Weight gradient of that layer from the rows it read, the 8-bit store a program keeps for its backward pass:
+ *   dw[m, n] = sum_t dy[t, m] x[t, n]  (fp32; products of bf16 operands, which hold 8-bit values exactly down to 2^-126).
+ *   dy, dys  dev, dys NULL: bf16 [T_cap, n_out] of row stride dy_row_stride; else 8-bit rows, dy_row_stride = n_out.  Read.
+ *   xq, xs   dev, 8-bit rows [T_cap, n_in], read.
+ *   dw       dev, [n_out, n_in] float, written (zeros if T = 0).
+ *   workspace  dev, at least mb_linear_fp8_wgrad_workspace_bytes bytes, scratch; may be NULL if that is 0.
+ * Deterministic: sums over tokens are taken in a fixed order that depends on the sizes (T_cap among them) only.
+ */
+MB_API size_t mb_linear_fp8_wgrad_workspace_bytes(int T_cap, int n_in, int n_out);
+MB_API mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy_row_stride, const uint8_t* xq,
+                                     const uint8_t* xs, int T_cap, const int32_t* meta_dev, int n_in, int n_out, float* dw,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The GeGLU feed-forward on 8-bit rows, the parts around its gate (the second projection and the other products are
+ * mb_linear_fp8_fwd and mb_linear_fp8_wgrad):
+ *
+ * mb_geglu_fp8_act      act = GeLU(x W1) (*) x V, fp32 up to the store in 8 bits; neither projection is written to memory.
+ *   xq, xs      dev, rows [T_cap, hidden], read.
+ *   w1vq, w1vs  dev, weight [2*inter, hidden], W1 transposed over V transposed as in mb_geglu_fwd, read.
+ *   actq, acts  dev, rows [T_cap, inter], written.
+ * mb_gelu_gate_fp8_bwd  dh = dA (*) g (*) GeLU'(h),  dg = dA (*) GeLU(h), stored as the rows dh | dg.
+ *   da          dev, bf16 [T_cap, inter], read.
+ *   hg, hgs     dev, h | g [T_cap, 2*inter]: bf16 with hgs NULL (x (W1 | V) by mb_linear_fp8_fwd), or 8-bit rows.  Read.
+ *   dhgq, dhgs  dev, rows [T_cap, 2*inter], written.
+ * inter is a multiple of 128 (MB_ERR_UNSUPPORTED otherwise), 2 * inter * hidden < 2^31.
+ */
+MB_API mb_status mb_geglu_fp8_act(const uint8_t* xq, const uint8_t* xs, const uint8_t* w1vq, const uint8_t* w1vs, int T_cap,
+                                  const int32_t* meta_dev, int hidden, int inter, uint8_t* actq, uint8_t* acts, void* stream);
+MB_API mb_status mb_gelu_gate_fp8_bwd(const void* da, const void* hg, const uint8_t* hgs, int T_cap, const int32_t* meta_dev,
+                                      int inter, uint8_t* dhgq, uint8_t* dhgs, void* stream);
+
+/*
  * Ceiling probe for callers that measure (bench.py): enqueues one launch of a kernel that saturates one unit
  * and does nothing else, and reports the work of that launch; the caller times it.  Not an operation of the
  * paper: it exists so that the roofs kernels are priced against are measured on the machine at hand.

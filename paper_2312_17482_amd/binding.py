@@ -32,7 +32,9 @@ EXPORTS = ("mb_last_error", "mb_version", "mb_alibi_slopes", "mb_unpad_index", "
            "mb_alibi_attn_bwd_workspace_bytes",
            "mb_alibi_attn_bwd", "mb_add_layernorm_fwd", "mb_add_layernorm_bwd_workspace_bytes",
            "mb_add_layernorm_bwd", "mb_geglu_fwd", "mb_geglu_bwd_workspace_bytes", "mb_geglu_bwd", "mb_linear_fwd", "mb_gelu_gate", "mb_probe_ceiling",
-           "mb_alibi_attn_bwd_static", "mb_device_status", "mb_attn_plan_bytes", "mb_attn_plan", "mb_probe_bwd_traffic")
+           "mb_alibi_attn_bwd_static", "mb_device_status", "mb_attn_plan_bytes", "mb_attn_plan", "mb_probe_bwd_traffic",
+           "mb_fp8_quant", "mb_fp8_dequant", "mb_fp8_quant_weight", "mb_linear_fp8_fwd", "mb_linear_fp8_wgrad_workspace_bytes",
+           "mb_linear_fp8_wgrad", "mb_geglu_fp8_act", "mb_gelu_gate_fp8_bwd")
 
 _lib.mb_last_error.restype = c_char_p
 _lib.mb_last_error.argtypes = []
@@ -98,6 +100,25 @@ _lib.mb_gelu_gate.argtypes = [c_void_p, c_void_p, c_int64, c_int, c_void_p, c_in
 _lib.mb_geglu_fwd.restype = c_int
 _lib.mb_geglu_fwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_void_p, c_void_p,
                               c_void_p]
+_lib.mb_fp8_quant.restype = c_int
+_lib.mb_fp8_quant.argtypes = [c_void_p, c_int64, c_int, c_void_p, c_int, c_int, c_void_p, c_void_p, c_void_p]
+_lib.mb_fp8_dequant.restype = c_int
+_lib.mb_fp8_dequant.argtypes = [c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_void_p, c_int64, c_void_p]
+_lib.mb_fp8_quant_weight.restype = c_int
+_lib.mb_fp8_quant_weight.argtypes = [c_void_p, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+_lib.mb_linear_fp8_fwd.restype = c_int
+_lib.mb_linear_fp8_fwd.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_int, c_void_p,
+                                   c_int64, c_void_p]
+_lib.mb_linear_fp8_wgrad_workspace_bytes.restype = c_size_t
+_lib.mb_linear_fp8_wgrad_workspace_bytes.argtypes = [c_int, c_int, c_int]
+_lib.mb_linear_fp8_wgrad.restype = c_int
+_lib.mb_linear_fp8_wgrad.argtypes = [c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_void_p,
+                                     c_void_p, c_size_t, c_void_p]
+_lib.mb_geglu_fp8_act.restype = c_int
+_lib.mb_geglu_fp8_act.argtypes = [c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_int, c_void_p, c_void_p,
+                                  c_void_p]
+_lib.mb_gelu_gate_fp8_bwd.restype = c_int
+_lib.mb_gelu_gate_fp8_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_int, c_void_p, c_void_p, c_void_p]
 
 
 class MosaicAttnError(RuntimeError):
@@ -159,20 +180,25 @@ def _load_calls():
         raise ImportError("%s does not load with torch %s; it was built for another one, or not whole. %s"
                           % (_MARSHAL_PATH, torch.__version__, _HOW_TO_BUILD)) from e
     addresses = {name: ctypes.cast(getattr(_lib, name), c_void_p).value for name in EXPORTS}
-    return native.Calls(addresses, MosaicAttnError, getattr(torch._C, "_cuda_getDevice", _current_device), _raw_stream,
-                        _stream)
+    host = (addresses, MosaicAttnError, getattr(torch._C, "_cuda_getDevice", _current_device), _raw_stream, _stream)
+    return native.Calls(*host), native.Fp8Calls(*host)
 
 
 # Host time of a whole layer step of 8 x 128 positions, eight calls (33 us of kernels): 60 us with these calls marshalled in
 # Python; see csrc/marshal.cpp.
-_calls = _load_calls()
+_calls, _fp8_calls = _load_calls()
 
 
 def _calls_of_this_module():
     return _calls
 
 
+def _fp8_calls_of_this_module():
+    return _fp8_calls
+
+
 copyreg.pickle(type(_calls), lambda _: (_calls_of_this_module, ()))   # its methods pickle by name, as functions do
+copyreg.pickle(type(_fp8_calls), lambda _: (_fp8_calls_of_this_module, ()))
 
 mb_unpad_index = _calls.mb_unpad_index
 mb_unpad = _calls.mb_unpad
@@ -185,6 +211,13 @@ mb_add_layernorm_bwd = _calls.mb_add_layernorm_bwd
 mb_geglu_fwd = _calls.mb_geglu_fwd
 mb_geglu_bwd = _calls.mb_geglu_bwd
 mb_linear_fwd = _calls.mb_linear_fwd
+mb_fp8_quant = _fp8_calls.mb_fp8_quant
+mb_fp8_dequant = _fp8_calls.mb_fp8_dequant
+mb_fp8_quant_weight = _fp8_calls.mb_fp8_quant_weight
+mb_linear_fp8_fwd = _fp8_calls.mb_linear_fp8_fwd
+mb_linear_fp8_wgrad = _fp8_calls.mb_linear_fp8_wgrad
+mb_geglu_fp8_act = _fp8_calls.mb_geglu_fp8_act
+mb_gelu_gate_fp8_bwd = _fp8_calls.mb_gelu_gate_fp8_bwd
 
 
 def mb_version() -> int:
@@ -287,3 +320,7 @@ def mb_probe_bwd_traffic(qkv, dout, o, dqkv, cu_seqlens) -> None:
 
 def mb_geglu_bwd_workspace_bytes(T_cap: int, hidden: int, inter: int, dtype_code: int = MB_BF16) -> int:
     return int(_lib.mb_geglu_bwd_workspace_bytes(T_cap, hidden, inter, dtype_code))
+
+
+def mb_linear_fp8_wgrad_workspace_bytes(T_cap: int, n_in: int, n_out: int) -> int:
+    return int(_lib.mb_linear_fp8_wgrad_workspace_bytes(T_cap, n_in, n_out))

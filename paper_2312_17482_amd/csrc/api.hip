@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 
+#include "api_check.h"
 #include "common.h"
 
 // Device-resident state of the library (one copy per GPU, held until the process ends):
@@ -77,22 +78,6 @@ mb_status check_launch(const char* what) {
 }
 
 namespace {
-
-#define MB_REQUIRE(cond, code, ...) \
-  do {                              \
-    if (!(cond)) return fail(code, __VA_ARGS__); \
-  } while (0)
-
-mb_status check_ptr(const void* p, const char* name) {
-  MB_REQUIRE(p != nullptr, MB_ERR_INVALID_ARG, "%s is NULL", name);
-  MB_REQUIRE(aligned16(p), MB_ERR_INVALID_ARG, "%s is not 16-byte aligned", name);
-  return MB_OK;
-}
-#define MB_CHECK_PTR(p)                              \
-  do {                                               \
-    const mb_status st_ = check_ptr((p), #p);        \
-    if (st_ != MB_OK) return st_;                    \
-  } while (0)
 
 mb_status check_dtype(mb_dtype dt) {
   MB_REQUIRE(dt == MB_F32 || dt == MB_BF16, MB_ERR_INVALID_ARG, "unknown dtype %d", (int)dt);

@@ -108,6 +108,25 @@ mb_status launch_add_layernorm_bwd(mb_dtype dt, const void* dy, const void* s, c
                                    const float* rstd, int T_cap, const int32_t* meta, int W, void* ds, float* dgamma,
                                    float* dbeta, float* part, const int32_t* dy_rows, hipStream_t stream);
 
+// 8-bit rows and weights (fp8_util.h says what they are).
+mb_status launch_fp8_quant(mb_dtype dt, const void* x, int64_t stride, int T_cap, const int32_t* meta, int W, uint8_t* q,
+                           uint8_t* s, hipStream_t stream);
+mb_status launch_fp8_dequant(mb_dtype dt, const uint8_t* q, const uint8_t* s, int T_cap, const int32_t* meta, int W, void* x,
+                             int64_t stride, hipStream_t stream);
+mb_status launch_fp8_quant_weight(mb_dtype dt, const void* w, int n_out, int n_in, uint8_t* q, uint8_t* s, uint8_t* qt,
+                                  uint8_t* st, hipStream_t stream);
+mb_status launch_gelu_gate_fp8_bwd(const void* da, const void* hg, const uint8_t* hgs, int T_cap, const int32_t* meta,
+                                   int inter, uint8_t* q, uint8_t* s, hipStream_t stream);
+mb_status launch_linear_fp8_fwd(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, int T_cap,
+                                const int32_t* meta, int n_in, int n_out, mb_dtype y_dt, void* y, int64_t y_row_stride,
+                                hipStream_t stream);
+mb_status launch_geglu_fp8_act(const uint8_t* xq, const uint8_t* xs, const uint8_t* w1vq, const uint8_t* w1vs, int T_cap,
+                               const int32_t* meta, int hidden, int inter, uint8_t* actq, uint8_t* acts, hipStream_t stream);
+size_t linear_fp8_wgrad_workspace_bytes(int T_cap, int n_in, int n_out);
+mb_status launch_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy_row_stride, const uint8_t* xq,
+                                  const uint8_t* xs, int T_cap, const int32_t* meta, int n_in, int n_out, float* dw,
+                                  void* workspace, hipStream_t stream);
+
 // Generic kernels: any D <= 128, fp32 or bf16 storage, fp32 arithmetic.  Longer promises are refused (part of the
 // calls' contract; the kernels themselves stream their keys and have no such limit).
 static constexpr int kGenericMaxSeqlen = 8000;

@@ -1,0 +1,106 @@
+// 8-bit rows: e4m3 (OCP: 4 bits of exponent, 3 of mantissa, largest value 448, no infinity) with one scale for each block of
+// 128 values of a row, or for each 128 x 128 block of a weight.  A scale is a power of two, kept as its exponent's byte b: 2^(b - 127).
+// Powers of two because they cost nothing: dividing by one and multiplying by one round nothing, a stored value times its scale
+// is exact in bf16, and the matrix instruction takes the byte as it is.
+#pragma once
+#include "common.h"
+#include "mfma_util.h"
+
+namespace mb {
+
+constexpr int kFp8Block = 128;
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+__host__ __device__ inline int fp8_blocks(int width) { return (width + kFp8Block - 1) / kFp8Block; }
+
+// Descriptor of `bytes` bytes from `base`, both the same in all lanes.  (Said to the compiler word by word: bounds that it works out
+// on the vector unit would make a loop over the lanes of every access.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t uniform_rsrc(const void* base, uint32_t bytes) {
+  const uint64_t a = reinterpret_cast<uint64_t>(base);
+  const uint64_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)a), hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(a >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(hi << 32 | lo), 0,
+                                           (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000);
+}
+
+// |x|, or 0 for infinities and NaN (which a block's scale is not taken from).
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = fabsf(x);
+  return a < __builtin_inff() ? a : 0.f;
+}
+
+// The scale of a block whose largest finite magnitude is `amax`: the smallest 2^e, e >= -126, with amax <= 448 * 2^e, as e + 127.
+// (448 = 1.75 * 2^8: the addition carries into the exponent where the mantissa is over 1.75.)
+__device__ __forceinline__ int scale_byte(float amax) {
+  return max((int)((__float_as_uint(amax) + 0x1fffffu) >> 23) - 8, 1);
+}
+// 1 / scale, exact; bytes 1 .. 247.
+__device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+// The scale itself; byte 255 stands for NaN.
+__device__ __forceinline__ float scale_value(int byte) {
+  return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)byte << 23);
+}
+
+// Four values, already divided by their scale, as e4m3 (round to nearest even; what is not finite becomes NaN).
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+}
+// Four e4m3 values.
+__device__ __forceinline__ void unpack_e4m3(uint32_t w, float (&x)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  x[0] = lo[0];
+  x[1] = lo[1];
+  x[2] = hi[0];
+  x[3] = hi[1];
+}
+
+// Eight e4m3 values times a scale, as bf16; exact where the product is a normal number.  (Of `scale` the instruction takes the
+// exponent: byte << 23 as a float.)
+__device__ __forceinline__ bf16x8 to_bf16x8(uint32_t lo, uint32_t hi, float scale) {
+  u32x4 r;
+  r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, false));
+  r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, scale, true));
+  r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, false));
+  r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, scale, true));
+  return as_bf16x8(r);
+}
+
+// Largest of a value over groups of 8 consecutive lanes (the 8 lanes that hold a block of a row, 16 values each).
+__device__ __forceinline__ float max_of_8_lanes(float x) {
+  x = fmaxf(x, __shfl_xor(x, 1));
+  x = fmaxf(x, __shfl_xor(x, 2));
+  return fmaxf(x, __shfl_xor(x, 4));
+}
+
+// Phi(-|h|) and exp(-h^2 / 2) for the GeLU, Phi the normal distribution function.  With x = |h| / sqrt 2:
+//   Phi(-|h|) = erfc(x) / 2 = t P(t) exp(-x^2) / 2,  t = 1 / (1 + 0.38 x),
+// P of degree 6 through erfc(x) exp(x^2) / t, fitted for the least RELATIVE error over x = 0 .. 9.5 (1.0e-6; 3e-6 with fp32
+// arithmetic up to |h| = 6, 7e-6 up to 12).  Relative, because a block whose gates are all far negative gets a scale of its own: there an
+// absolute error of 1e-7, enough for a bf16 result next to larger ones, would be most of the value.
+__device__ __forceinline__ float normal_tail(float h, float& e) {
+  const float ah = fabsf(h);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.38f * 0.70710678118654752f, ah, 1.0f));
+  float p = fmaf(0.5f * -0.1250446775797289f, t, 0.5f * 0.3346000856655536f);
+  p = fmaf(p, t, 0.5f * -0.0676826123937758f);
+  p = fmaf(p, t, 0.5f * 0.2460534679856757f);
+  p = fmaf(p, t, 0.5f * 0.1813618473996311f);
+  p = fmaf(p, t, 0.5f * 0.2164089138960925f);
+  p = fmaf(p, t, 0.5f * 0.2143019639678111f);
+  e = __builtin_amdgcn_exp2f(h * h * (-0.5f * kLog2e));
+  return p * t * e;
+}
+// GeLU(h) = h Phi(h), and its derivative Phi(h) + h phi(h).
+__device__ __forceinline__ float gelu_tail(float h) {
+  float e;
+  const float u = normal_tail(h, e);
+  return h * (h < 0.f ? u : 1.0f - u);
+}
+__device__ __forceinline__ void gelu_tail_and_grad(float h, float& val, float& grad) {
+  float e;
+  const float u = normal_tail(h, e);
+  const float cdf = h < 0.f ? u : 1.0f - u;
+  val = h * cdf;
+  grad = fmaf(h * 0.3989422804014327f, e, cdf);
+}
+
+}  // namespace mb

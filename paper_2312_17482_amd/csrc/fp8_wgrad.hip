@@ -1,0 +1,263 @@
+// Weight gradient from 8-bit rows:  dw[m, n] = sum over tokens t of dy[t, m] x[t, n], x the e4m3 rows that the product read (and
+// the program kept), dy bf16 or e4m3 rows, fp32 sums.
+//
+// The contraction runs over tokens, along which every block has a scale of its own: the scaled matrix instruction, one byte for 32
+// of k, cannot take them.  So the operands are brought back to bf16 on their way into LDS (v_cvt_scalef32_pk_bf16_fp8, exact: 4
+// bits of significand and a power of two) and multiplied by v_mfma_f32_32x32x16_bf16.  They pass through registers for it: 16 bytes of
+// a row per load, one scale byte each, two 16-byte LDS writes.  The rest is the bf16 weight gradient's way: rows as they are
+// in LDS, operands by transposing reads, 64 kMB x 256 tiles by 8 waves, steps of 64 tokens in two stages, the tokens split over
+// workgroups where the tiles are few, partial tiles added in a fixed order.
+#include "fp8_util.h"
+
+namespace mb {
+namespace {
+
+constexpr int kRows = 64;         // tokens per step
+constexpr int kMaxSplits = 32;
+
+struct Wgrad {
+  const void* dy;                 // bf16 [T, n_out] of row stride dy_stride, or e4m3 with scales dys
+  const uint8_t* dys;
+  int64_t dy_stride;
+  const uint8_t *x, *xs;
+  int n_out, n_in, n_tiles, tiles, splits, T_cap;
+  const int32_t* meta;
+  float* out;                     // of the first split; split s is n_out n_in floats further on, s times
+};
+
+// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.  Piece x (8 bf16 columns) of row r
+// sits at position x ^ 4 (r % 4): the four rows a transposing read touches lie in different banks.
+template <bool kEight, int kCols>
+struct Stager {
+  static constexpr int kPerRow = kCols / (kEight ? 16 : 8);   // 16-byte pieces of a row in memory
+  static constexpr int kN = kRows * kPerRow / 512;            // per thread
+  u32x4 data[kN];
+  uint8_t byte[kN];
+  int row, piece;
+  uint32_t off, soff;       // byte offsets in a step's rows (out of range where the columns end)
+  const uint8_t *base, *sbase;
+  int64_t pitch;            // bytes from row to row
+  int blocks, T;
+  __device__ __forceinline__ Stager(const void* p, const uint8_t* s, int64_t stride, int first_col, int cols, int T_, int tid) {
+    constexpr int kEs = kEight ? 1 : 2;
+    row = tid / kPerRow;
+    piece = tid % kPerRow;
+    pitch = stride * kEs;
+    blocks = fp8_blocks(cols);
+    T = T_;
+    const int col = piece * (16 / kEs);
+    const bool there = first_col + col < cols;
+    base = static_cast<const uint8_t*>(p) + (int64_t)first_col * kEs;
+    sbase = kEight ? s : nullptr;
+    off = there ? (uint32_t)row * (uint32_t)pitch + piece * 16 : 0x80000000u;
+    soff = there ? (uint32_t)row * (uint32_t)blocks + (first_col + col) / kFp8Block : 0x80000000u;
+  }
+  // requests the rows of 64 tokens from `first` on (rows at or beyond T: zeros)
+  __device__ __forceinline__ void request(int first) {
+    const int rows = max(min(T - first, kRows), 0);
+    const int at = rows > 0 ? first : 0;
+    const __amdgpu_buffer_rsrc_t r = uniform_rsrc(base + (int64_t)at * pitch, (uint32_t)rows * (uint32_t)pitch);
+#pragma unroll
+    for (int i = 0; i < kN; ++i)
+      data[i] = __builtin_amdgcn_raw_buffer_load_b128(r, off, (uint32_t)(i * (512 / kPerRow)) * (uint32_t)pitch, 0);
+    if (kEight) {
+      const __amdgpu_buffer_rsrc_t q = uniform_rsrc(sbase + (int64_t)at * blocks, (uint32_t)rows * (uint32_t)blocks);
+#pragma unroll
+      for (int i = 0; i < kN; ++i)
+        byte[i] = __builtin_amdgcn_raw_buffer_load_b8(q, soff, (uint32_t)(i * (512 / kPerRow)) * (uint32_t)blocks, 0);
+    }
+  }
+  // brings the i-th of what was requested to LDS
+  __device__ __forceinline__ void put(uint16_t* to, int i) const {
+    const int r = row + i * (512 / kPerRow);
+    uint16_t* const at = to + r * kCols;
+    if (kEight) {
+      const float scale = __uint_as_float((uint32_t)byte[i] << 23);
+      *reinterpret_cast<bf16x8*>(at + ((2 * piece) ^ (4 * (r & 3))) * 8) = to_bf16x8(data[i][0], data[i][1], scale);
+      *reinterpret_cast<bf16x8*>(at + ((2 * piece + 1) ^ (4 * (r & 3))) * 8) = to_bf16x8(data[i][2], data[i][3], scale);
+    } else {
+      *reinterpret_cast<u32x4*>(at + (piece ^ (4 * (r & 3))) * 8) = data[i];
+    }
+  }
+};
+
+template <bool kEight, int kMB>
+__global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
+  constexpr int kM = 64 * kMB, kStage = kRows * (kM + 256), kMfma = 2 * kMB, kFrags = kMB + 2;
+  __shared__ __attribute__((aligned(1024))) uint16_t smem[2 * kStage];
+  const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
+  // workgroup -> split and tile, every XCD a contiguous run: its compute units stream the same token rows
+  const int total = pr.tiles * pr.splits, run = total >> 3;
+  int lin = blockIdx.x;
+  if (lin < (run << 3)) lin = (lin & 7) * run + (lin >> 3);
+  const int split = __builtin_amdgcn_readfirstlane(lin / pr.tiles);
+  const int tile = __builtin_amdgcn_readfirstlane(lin - split * pr.tiles);
+  const int tile_m = __builtin_amdgcn_readfirstlane(tile / pr.n_tiles);
+  const int m0 = tile_m * kM, n0 = (tile - tile_m * pr.n_tiles) * 256;
+  const int steps_total = (T + kRows - 1) / kRows;
+  const int per = __builtin_amdgcn_readfirstlane((steps_total + pr.splits - 1) / pr.splits);
+  const int begin = split * per;
+  const int nsteps = max(min(steps_total - begin, per), 0);
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c = lane & 31, g = lane >> 5;
+  const int wm = wave >> 2, wn = wave & 3;
+  Stager<kEight, kM> ps(pr.dy, pr.dys, pr.dy_stride, m0, pr.n_out, T, tid);
+  Stager<true, 256> qs(pr.x, pr.xs, pr.n_in, n0, pr.n_in, T, tid);
+
+  // Fragment reads: lane -> row tr_row (+ 8) and 4 columns of a 16 x 32 patch; P columns 32 (kMB wm + mb), Q columns
+  // 64 wn + 32 nb.
+  const int tr_i = lane & 15, tr_q = lane >> 4;
+  const int tr_row = (tr_i >> 2) + 4 * (tr_q >> 1);
+  const int tr_piece = 2 * (tr_q & 1) + ((tr_i & 3) >> 1), tr_sub = 4 * (tr_i & 1);
+  uint32_t foff[kFrags];
+#pragma unroll
+  for (int i = 0; i < kFrags; ++i) {
+    const int x = (i < kMB ? 4 * (kMB * wm + i) : 8 * wn + 4 * (i - kMB)) + tr_piece;
+    foff[i] = (i < kMB ? 0 : kRows * kM) + tr_row * (i < kMB ? kM : 256) + ((x ^ (4 * (tr_i >> 2))) * 8) + tr_sub;
+  }
+  bf16x8 pf[2][kMB], qf[2][2];
+  auto read_frag = [&](int stage, int kk, int i) {
+    const int cols = i < kMB ? kM : 256;
+    const uint16_t* p = smem + stage * kStage + foff[i] + kk * (16 * cols);
+    const bf16x8 f = join_tr(lds_read_tr4(p), lds_read_tr4(p + 8 * cols));
+    if (i < kMB) pf[kk & 1][i] = f;
+    else qf[kk & 1][i - kMB] = f;
+  };
+  constexpr int kPuts = Stager<kEight, kM>::kN + Stager<true, 256>::kN;
+  auto put = [&](int stage, int i) {
+    if (i < qs.kN) qs.put(smem + stage * kStage + kRows * kM, i);
+    else ps.put(smem + stage * kStage, i - qs.kN);
+  };
+  auto request = [&](int step) {
+    qs.request((begin + step) * kRows);
+    ps.request((begin + step) * kRows);
+  };
+  f32x16 acc[kMB][2];   // [m block][n block]
+#pragma unroll
+  for (int x = 0; x < kMB; ++x)
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.f;
+
+  request(0);
+#pragma unroll
+  for (int i = 0; i < kPuts; ++i) put(0, i);
+  request(1);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kFrags; ++i) read_frag(0, 0, i);
+  // A step is four quarters of 16 tokens; during a quarter the next one's fragments are read.  In the first half the step
+  // after this one, requested a step ago, goes to the other stage, and the one behind it is requested.  In front of the last
+  // quarter stands the barrier behind which the other stage is whole and this one is read no more.  (Steps past the last
+  // read zeros that nobody uses.)
+#pragma unroll 1
+  for (int st = 0; st < nsteps; ++st) {
+    const int stage = st & 1, next = stage ^ 1;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      if (kk == 2) request(st + 2);
+      if (kk == 3) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+#pragma unroll
+      for (int x = 0; x < kMfma; ++x) {
+#pragma unroll
+        for (int i = x; i < kFrags; i += kMfma) read_frag(kk == 3 ? next : stage, (kk + 1) & 3, i);
+        if (kk < 2) {
+#pragma unroll
+          for (int i = kk * kMfma + x; i < kPuts; i += 2 * kMfma) put(next, i);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        acc[x >> 1][x & 1] = mfma32(pf[kk & 1][x >> 1], qf[kk & 1][x & 1], acc[x >> 1][x & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // fp32 tile: register v of block (x, y) is row 8 (v / 4) + 4 g + v % 4, lane c is the column
+  const int row0 = m0 + wm * (32 * kMB);
+  float* const dst = pr.out + (int64_t)split * pr.n_out * pr.n_in + (int64_t)min(row0, pr.n_out) * pr.n_in;
+  const __amdgpu_buffer_rsrc_t ors = uniform_rsrc(dst, (uint32_t)max(min(pr.n_out - row0, 32 * kMB), 0) * (uint32_t)pr.n_in * 4u);
+#pragma unroll
+  for (int y = 0; y < 2; ++y) {
+    const int col = n0 + wn * 64 + y * 32 + c;
+    const uint32_t at = col < pr.n_in ? ((uint32_t)(4 * g) * (uint32_t)pr.n_in + col) * 4u : 0x80000000u;
+#pragma unroll
+    for (int x = 0; x < kMB; ++x)
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(acc[x][y][v]), ors, at,
+                                              (uint32_t)(x * 32 + 8 * (v >> 2) + (v & 3)) * (uint32_t)pr.n_in * 4u, 0);
+  }
+}
+
+// out[i] = sum over splits of partial[s][i], in order, four at a time.
+__global__ __launch_bounds__(256) void fp8_wgrad_add_kernel(const float* __restrict__ partial, int splits, int64_t count4,
+                                                            float* __restrict__ out) {
+  const float4* src = reinterpret_cast<const float4*>(partial);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count4; i += (int64_t)gridDim.x * 256) {
+    float4 a = src[i];
+    for (int s = 1; s < splits; ++s) {
+      const float4 b = src[(int64_t)s * count4 + i];
+      a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+    }
+    reinterpret_cast<float4*>(out)[i] = a;
+  }
+}
+
+// Splits of the tokens and the tile's height with the least estimated time.
+struct Choice {
+  int splits, height;
+};
+Choice choose(int T_cap, int n_in, int n_out) {
+  const int steps = (T_cap + kRows - 1) / kRows;
+  const double bytes = 4.0 * n_in * n_out;
+  Choice best{1, 4};
+  double least = 1e300;
+  for (int mb = 4; mb >= 2; mb -= 2) {
+    const int64_t tiles = (int64_t)((n_out + 64 * mb - 1) / (64 * mb)) * ((n_in + 255) / 256);
+    for (int s = 1; s <= kMaxSplits && s <= (steps > 0 ? steps : 1); ++s) {
+      const double cost = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits) * ((mb == 4 ? 1.5 : 1.1) * ((steps + s - 1) / s) + 6.0) +
+                          (s > 1 ? 4.0 + (2 * s + 1) * bytes / 4.5e6 : 0.0);
+      if (cost < least) {
+        least = cost;
+        best = Choice{s, mb};
+      }
+    }
+  }
+  return best;
+}
+
+template <bool kEight>
+void launch_wgrad(const Wgrad& pr, int height, hipStream_t stream) {
+  const dim3 grid((unsigned)(pr.tiles * pr.splits));
+  if (height == 4) fp8_wgrad_kernel<kEight, 4><<<grid, dim3(512), 0, stream>>>(pr);
+  else fp8_wgrad_kernel<kEight, 2><<<grid, dim3(512), 0, stream>>>(pr);
+}
+
+}  // namespace
+
+size_t linear_fp8_wgrad_workspace_bytes(int T_cap, int n_in, int n_out) {
+  const Choice ch = choose(T_cap, n_in, n_out);
+  return ch.splits > 1 ? (size_t)ch.splits * n_in * n_out * sizeof(float) : 0;
+}
+
+mb_status launch_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy_row_stride, const uint8_t* xq,
+                                  const uint8_t* xs, int T_cap, const int32_t* meta, int n_in, int n_out, float* dw,
+                                  void* workspace, hipStream_t stream) {
+  const Choice ch = choose(T_cap, n_in, n_out);
+  const int n_tiles = (n_in + 255) / 256, tiles = (n_out + 64 * ch.height - 1) / (64 * ch.height) * n_tiles;
+  const bool whole = ch.splits == 1;
+  const Wgrad pr{dy, dys, dy_row_stride, xq, xs, n_out, n_in, n_tiles, tiles, ch.splits, T_cap, meta,
+                 whole ? dw : static_cast<float*>(workspace)};
+  if (dys) launch_wgrad<true>(pr, ch.height, stream);
+  else launch_wgrad<false>(pr, ch.height, stream);
+  if (!whole) {
+    const int64_t count4 = (int64_t)n_in * n_out / 4;
+    fp8_wgrad_add_kernel<<<dim3((unsigned)(count4 < 2048 * 256 ? (count4 + 255) / 256 : 2048)), dim3(256), 0, stream>>>(
+        static_cast<const float*>(workspace), ch.splits, count4, dw);
+  }
+  return check_launch("fp8_wgrad_kernel");
+}
+
+}  // namespace mb

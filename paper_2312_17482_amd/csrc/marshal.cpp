@@ -2,18 +2,20 @@
 // code only.  With small batches the host's time per call is what bounds a step: in Python a call cost 1.5 to 4 us on top of
 // the launch, most of it for looking at tensors (data_ptr, shape, stride) one method call at a time.
 //
-// One object (`Calls`) per imported binding: it holds the addresses of the C functions, the binding's error class and how to
-// find the current stream.  Its methods take what the binding documents, by position or by name, and do what the C ABI does
+// Two objects (`Calls`, and `Fp8Calls` with the 8-bit calls) per imported binding, each of which holds the addresses of the C functions, the binding's error class and how to
+// find the current stream.  Their methods take what the binding documents, by position or by name, and do what the C ABI does
 // not: defaults, allocation of what is not given, and the checks of shapes and strides that are left once a tensor is a pointer.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
 #include <cstdint>
+#include <functional>
 #include <utility>
 
 #include "mosaic_attn.h"
@@ -31,13 +33,17 @@ void require(bool ok, const char* text) {
   if (!ok) raise(PyExc_AssertionError, text);
 }
 
-struct Calls {
+// What every object of calls holds.
+struct Host {
   PyObject_HEAD
   PyObject* error;        // the binding's exception class: (status, message)
   PyObject* device;       // () -> current device
   PyObject* raw_stream;   // (device) -> stream handle, or None
   PyObject* stream;       // () -> stream handle, where there is no raw_stream
   decltype(&mb_last_error) last_error;
+};
+
+struct Calls : Host {
   decltype(&mb_unpad_index) unpad_index;
   decltype(&mb_unpad) unpad;
   decltype(&mb_pad) pad;
@@ -53,6 +59,18 @@ struct Calls {
   decltype(&mb_geglu_bwd) geglu_bwd;
   decltype(&mb_geglu_bwd_workspace_bytes) geglu_bwd_bytes;
   decltype(&mb_linear_fwd) linear_fwd;
+};
+
+// The 8-bit calls.
+struct Fp8Calls : Host {
+  decltype(&mb_fp8_quant) quant;
+  decltype(&mb_fp8_dequant) dequant;
+  decltype(&mb_fp8_quant_weight) quant_weight;
+  decltype(&mb_linear_fp8_fwd) linear;
+  decltype(&mb_linear_fp8_wgrad) wgrad;
+  decltype(&mb_linear_fp8_wgrad_workspace_bytes) wgrad_bytes;
+  decltype(&mb_geglu_fp8_act) act;
+  decltype(&mb_gelu_gate_fp8_bwd) gate_bwd;
 };
 
 // ---------------------------------------------------------------------------------------------------- arguments
@@ -226,7 +244,7 @@ at::Tensor new_like(const at::Tensor& like, at::IntArrayRef sizes, at::ScalarTyp
 }
 at::Tensor new_bytes(const at::Tensor& like, size_t n) { return new_like(like, {(int64_t)n}, at::kByte); }
 
-void* current_stream(const Calls* s) {
+void* current_stream(const Host* s) {
   PyObject* handle;
   if (s->raw_stream == Py_None) {
     handle = PyObject_CallNoArgs(s->stream);
@@ -245,7 +263,7 @@ void* current_stream(const Calls* s) {
 
 // Runs the C function without the interpreter's lock, as ctypes does.
 template <typename F, typename... A>
-void run(const Calls* s, F function, A... args) {
+void run(const Host* s, F function, A... args) {
   mb_status status;
   Py_BEGIN_ALLOW_THREADS
   status = function(args...);
@@ -485,23 +503,227 @@ PyObject* linear_fwd(Self s, Argv argv, Py_ssize_t n, PyObject* kw) {
   return y.take();
 }
 
+// ---------------------------------------------------------------------------------------------------- the 8-bit calls
+using Self8 = const Fp8Calls*;
+constexpr int64_t kBlock = 128;
+int64_t blocks_of(int64_t width) { return (width + kBlock - 1) / kBlock; }
+
+// Tensors of one call: on one device, which is the current one (its stream is what the call goes to).
+template <typename... T>
+void together(Self8 s, const at::Tensor& first, const T&... others) {
+  require(((others.device() == first.device()) && ...), "all tensors must be on one device");
+  if (!first.is_cuda()) return;
+  PyObject* r = PyObject_CallNoArgs(s->device);
+  if (!r) throw Raised();
+  const long device = PyLong_AsLong(r);
+  Py_DECREF(r);
+  if (device == -1 && PyErr_Occurred()) throw Raised();
+  require(device == first.get_device(), "the tensors must be on the current device");
+}
+
+void codes(const at::Tensor& q) {
+  require(q.scalar_type() == at::kFloat8_e4m3fn && q.dim() == 2 && q.is_contiguous(), "8-bit values must be a contiguous float8_e4m3fn matrix");
+}
+// 8-bit rows (or, block = 128, a weight) and their scales.
+void stored(const at::Tensor& q, const at::Tensor& s, int64_t block = 1) {
+  codes(q);
+  require(s.scalar_type() == at::kFloat8_e8m0fnu && s.dim() == 2 && s.is_contiguous() && s.size(0) == (q.size(0) + block - 1) / block &&
+              s.size(1) == blocks_of(q.size(1)),
+          "scales must be a contiguous float8_e8m0fnu matrix with one value for each block of 128");
+}
+at::Tensor new_codes(const at::Tensor& like, int64_t rows, int64_t width) { return new_like(like, {rows, width}, at::kFloat8_e4m3fn); }
+at::Tensor new_scales(const at::Tensor& like, int64_t rows, int64_t width) {
+  return new_like(like, {rows, blocks_of(width)}, at::kFloat8_e8m0fnu);
+}
+// [rows, W] view with dense rows: the row stride in elements.
+int64_t matrix_stride(const at::Tensor& t) {
+  require(t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1), "need a matrix with dense rows");
+  return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
+}
+template <int N>
+int rows_used(const Args<N>& a, int i, int64_t rows) {
+  const int T_cap = a.integer_or(i, rows);
+  require(T_cap <= rows, "T_cap is more rows than there are");
+  return T_cap;
+}
+template <int N>
+const int32_t* meta_of(const Args<N>& a, int i) { return (const int32_t*)a.ptr(i); }
+
+PyObject* quant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("x", "T_cap", "meta", "q", "s");
+  const Args<5> a("mb_fp8_quant", names, 1, argv, n, kw);
+  const at::Tensor& x = a.tensor(0);
+  const int64_t stride = matrix_stride(x), rows = x.size(0), W = x.size(1);
+  const int T_cap = rows_used(a, 1, rows);
+  const mb_dtype dt = (mb_dtype)dtype_code(x);
+  Result q(a, 3, [&] { return new_codes(x, rows, W); });
+  Result sc(a, 4, [&] { return new_scales(x, rows, W); });
+  stored(q.tensor(a, 3), sc.tensor(a, 4));
+  require(q.tensor(a, 3).size(0) >= T_cap && q.tensor(a, 3).size(1) == W, "q must have x's columns and as many rows as are used");
+  together(s, x, q.tensor(a, 3), sc.tensor(a, 4));
+  run(s, s->quant, (const void*)x.data_ptr(), stride, T_cap, meta_of(a, 2), (int)W, dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+      current_stream(s));
+  return tuple_of(q.take(), sc.take());
+}
+
+// A torch dtype argument, or bfloat16.
+template <int N>
+at::ScalarType type_or_bf16(const Args<N>& a, int i) {
+  if (!a.given(i)) return at::kBFloat16;
+  if (!THPDtype_Check(a.v[i])) raise(PyExc_TypeError, "dtype must be a torch.dtype");
+  return reinterpret_cast<THPDtype*>(a.v[i])->scalar_type;
+}
+
+PyObject* dequant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("q", "s", "dtype", "T_cap", "meta", "out");
+  const Args<6> a("mb_fp8_dequant", names, 2, argv, n, kw);
+  const at::Tensor &q = a.tensor(0), &sc = a.tensor(1);
+  stored(q, sc);
+  const int64_t rows = q.size(0), W = q.size(1);
+  const int T_cap = rows_used(a, 3, rows);
+  Result out(a, 5, [&] { return new_like(q, {rows, W}, type_or_bf16(a, 2)); });
+  const at::Tensor& o = out.tensor(a, 5);
+  const int64_t stride = matrix_stride(o);
+  require(o.size(0) >= T_cap && o.size(1) == W, "out must have q's columns and as many rows as are used");
+  require(!a.given(2) || o.scalar_type() == type_or_bf16(a, 2), "out is of another dtype");
+  together(s, q, sc, o);
+  run(s, s->dequant, (const uint8_t*)q.data_ptr(), (const uint8_t*)sc.data_ptr(), T_cap, meta_of(a, 4), (int)W,
+      (mb_dtype)dtype_code(o), out.ptr, stride, current_stream(s));
+  return out.take();
+}
+
+PyObject* quant_weight(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("w", "transposed", "q", "s", "qt", "st");
+  const Args<6> a("mb_fp8_quant_weight", names, 1, argv, n, kw);
+  const at::Tensor& w = a.tensor(0);
+  require(w.dim() == 2 && w.is_contiguous(), "w must be a contiguous matrix");
+  const int64_t n_out = w.size(0), n_in = w.size(1);
+  const int both = a.given(1) ? PyObject_IsTrue(a.v[1]) : 1;
+  if (both < 0) throw Raised();
+  const mb_dtype dt = (mb_dtype)dtype_code(w);
+  const bool given_t = a.given(4) || a.given(5);
+  require(both || !given_t, "qt and st are outputs of transposed=True");
+  Result q(a, 2, [&] { return new_codes(w, n_out, n_in); });
+  Result sc(a, 3, [&] { return new_scales(w, blocks_of(n_out), n_in); });
+  Result qt(a, 4, [&] { return new_codes(w, both ? n_in : 0, n_out); });
+  Result st(a, 5, [&] { return new_scales(w, both ? blocks_of(n_in) : 0, n_out); });
+  stored(q.tensor(a, 2), sc.tensor(a, 3), kBlock);
+  stored(qt.tensor(a, 4), st.tensor(a, 5), kBlock);
+  require(q.tensor(a, 2).sizes() == w.sizes(), "q must have w's shape");
+  require(!both || (qt.tensor(a, 4).size(0) == n_in && qt.tensor(a, 4).size(1) == n_out), "qt must have w's shape transposed");
+  together(s, w, q.tensor(a, 2), sc.tensor(a, 3), qt.tensor(a, 4), st.tensor(a, 5));
+  run(s, s->quant_weight, (const void*)w.data_ptr(), (int)n_out, (int)n_in, dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+      both ? (uint8_t*)qt.ptr : nullptr, both ? (uint8_t*)st.ptr : nullptr, current_stream(s));
+  if (!both) return tuple_of(q.take(), sc.take());
+  return tuple_of(q.take(), sc.take(), qt.take(), st.take());
+}
+
+PyObject* linear(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("xq", "xs", "wq", "ws", "dtype", "T_cap", "meta", "y");
+  const Args<8> a("mb_linear_fp8_fwd", names, 4, argv, n, kw);
+  const at::Tensor &xq = a.tensor(0), &xs = a.tensor(1), &wq = a.tensor(2), &ws = a.tensor(3);
+  stored(xq, xs);
+  stored(wq, ws, kBlock);
+  const int64_t rows = xq.size(0), n_in = xq.size(1), n_out = wq.size(0);
+  require(wq.size(1) == n_in, "the weight must have as many columns as the rows");
+  const int T_cap = rows_used(a, 5, rows);
+  Result y(a, 7, [&] { return new_like(xq, {rows, n_out}, type_or_bf16(a, 4)); });
+  const at::Tensor& o = y.tensor(a, 7);
+  const int64_t stride = matrix_stride(o);
+  require(o.size(0) >= T_cap && o.size(1) == n_out, "y must have the weight's rows as columns and as many rows as are used");
+  require(!a.given(4) || o.scalar_type() == type_or_bf16(a, 4), "y is of another dtype");
+  together(s, xq, xs, wq, ws, o);
+  run(s, s->linear, (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), (const uint8_t*)wq.data_ptr(),
+      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 6), (int)n_in, (int)n_out, (mb_dtype)dtype_code(o), y.ptr, stride,
+      current_stream(s));
+  return y.take();
+}
+
+PyObject* wgrad(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("dy", "xq", "xs", "dys", "T_cap", "meta", "dw", "workspace");
+  const Args<8> a("mb_linear_fp8_wgrad", names, 3, argv, n, kw);
+  const at::Tensor &dy = a.tensor(0), &xq = a.tensor(1), &xs = a.tensor(2);
+  const bool eight = a.given(3);
+  stored(xq, xs);
+  if (eight) stored(dy, a.tensor(3));
+  else require(dy.scalar_type() == at::kBFloat16, "dy must be bfloat16, or 8-bit rows with dys");
+  const int64_t stride = matrix_stride(dy), rows = xq.size(0), n_in = xq.size(1), n_out = dy.size(1);
+  const int T_cap = rows_used(a, 4, std::min(rows, dy.size(0)));
+  require(a.given(4) || dy.size(0) == rows, "dy must have as many rows as the stored ones");
+  Result dw(a, 6, [&] { return new_like(xq, {n_out, n_in}, at::kFloat); });
+  const at::Tensor& o = dw.tensor(a, 6);
+  require(o.scalar_type() == at::kFloat && o.dim() == 2 && o.is_contiguous() && o.size(0) == n_out && o.size(1) == n_in,
+          "dw must be a contiguous float32 matrix [columns of dy, columns of x]");
+  const size_t need = a.given(7) ? 0 : s->wgrad_bytes(T_cap, (int)n_in, (int)n_out);
+  Result workspace(a, 7, [&] { return new_bytes(xq, need); });
+  if (eight) together(s, dy, a.tensor(3), xq, xs, o);
+  else together(s, dy, xq, xs, o);
+  run(s, s->wgrad, (const void*)dy.data_ptr(), eight ? (const uint8_t*)a.ptr(3) : nullptr, eight ? n_out : stride,
+      (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), T_cap, meta_of(a, 5), (int)n_in, (int)n_out, (float*)dw.ptr,
+      workspace.ptr, workspace.numel(a, 7), current_stream(s));
+  return dw.take();
+}
+
+PyObject* geglu_act(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("xq", "xs", "w1vq", "w1vs", "T_cap", "meta", "actq", "acts");
+  const Args<8> a("mb_geglu_fp8_act", names, 4, argv, n, kw);
+  const at::Tensor &xq = a.tensor(0), &xs = a.tensor(1), &wq = a.tensor(2), &ws = a.tensor(3);
+  stored(xq, xs);
+  stored(wq, ws, kBlock);
+  const int64_t rows = xq.size(0), hidden = xq.size(1), inter = wq.size(0) / 2;
+  require(wq.size(1) == hidden && wq.size(0) % 2 == 0, "w1vq must be [2 * inter, columns of xq]");
+  const int T_cap = rows_used(a, 4, rows);
+  Result q(a, 6, [&] { return new_codes(xq, rows, inter); });
+  Result sc(a, 7, [&] { return new_scales(xq, rows, inter); });
+  stored(q.tensor(a, 6), sc.tensor(a, 7));
+  require(q.tensor(a, 6).size(0) >= T_cap && q.tensor(a, 6).size(1) == inter, "actq must have inter columns and as many rows as are used");
+  together(s, xq, xs, wq, ws, q.tensor(a, 6), sc.tensor(a, 7));
+  run(s, s->act, (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), (const uint8_t*)wq.data_ptr(),
+      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 5), (int)hidden, (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+      current_stream(s));
+  return tuple_of(q.take(), sc.take());
+}
+
+PyObject* gate_bwd(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
+  static const Names names("da", "hg", "hgs", "T_cap", "meta", "dhgq", "dhgs");
+  const Args<7> a("mb_gelu_gate_fp8_bwd", names, 2, argv, n, kw);
+  const at::Tensor &da = a.tensor(0), &hg = a.tensor(1);
+  const bool eight = a.given(2);
+  require(da.scalar_type() == at::kBFloat16 && da.dim() == 2 && da.is_contiguous(), "da must be a contiguous bfloat16 matrix");
+  if (eight) stored(hg, a.tensor(2));
+  else require(hg.scalar_type() == at::kBFloat16 && hg.dim() == 2 && hg.is_contiguous(), "hg must be contiguous bfloat16, or 8-bit rows with hgs");
+  const int64_t rows = da.size(0), inter = da.size(1);
+  require(hg.size(0) == rows && hg.size(1) == 2 * inter, "hg must be [rows of da, 2 * inter]");
+  const int T_cap = rows_used(a, 3, rows);
+  Result q(a, 5, [&] { return new_codes(da, rows, 2 * inter); });
+  Result sc(a, 6, [&] { return new_scales(da, rows, 2 * inter); });
+  stored(q.tensor(a, 5), sc.tensor(a, 6));
+  require(q.tensor(a, 5).size(0) >= T_cap && q.tensor(a, 5).size(1) == 2 * inter, "dhgq must have 2 * inter columns and as many rows as are used");
+  if (eight) together(s, da, hg, a.tensor(2), q.tensor(a, 5), sc.tensor(a, 6));
+  else together(s, da, hg, q.tensor(a, 5), sc.tensor(a, 6));
+  run(s, s->gate_bwd, (const void*)da.data_ptr(), (const void*)hg.data_ptr(), eight ? (const uint8_t*)a.ptr(2) : nullptr, T_cap,
+      meta_of(a, 4), (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr, current_stream(s));
+  return tuple_of(q.take(), sc.take());
+}
+
 // ---------------------------------------------------------------------------------------------------- the object
 // No C++ exception leaves a method.
-template <PyObject* (*F)(Self, Argv, Py_ssize_t, PyObject*)>
+template <typename C, PyObject* (*F)(const C*, Argv, Py_ssize_t, PyObject*)>
 PyObject* guarded(PyObject* self, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
   HANDLE_TH_ERRORS
   try {
-    return F(reinterpret_cast<const Calls*>(self), args, n, kw);
+    return F(reinterpret_cast<const C*>(self), args, n, kw);
   } catch (const Raised&) {
     return nullptr;
   }
   END_HANDLE_TH_ERRORS
 }
-template <PyObject* (*F)(Self, Argv, Py_ssize_t, PyObject*)>
+template <typename C, PyObject* (*F)(const C*, Argv, Py_ssize_t, PyObject*)>
 PyCFunction method() {
-  return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<F>));
+  return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&guarded<C, F>));
 }
-#define MB_METHOD(name, f, doc) {name, method<f>(), METH_FASTCALL | METH_KEYWORDS, doc}
+#define MB_METHOD(name, f, doc) {name, method<Calls, f>(), METH_FASTCALL | METH_KEYWORDS, doc}
+#define MB_METHOD8(name, f, doc) {name, method<Fp8Calls, f>(), METH_FASTCALL | METH_KEYWORDS, doc}
 
 PyMethodDef methods[] = {
     MB_METHOD("mb_unpad_index", unpad_index,
@@ -549,31 +771,36 @@ PyMethodDef methods[] = {
               "y = x @ wt.T for x [rows, n_in], wt [n_out, n_in]."),
     {nullptr, nullptr, 0, nullptr}};
 
-// Calls(addresses, error, device, raw_stream, stream): `addresses` maps names of the C ABI to function addresses.
-PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
-  PyObject *addresses, *error, *device, *raw_stream, *stream;
-  if (!PyArg_ParseTuple(args, "O!OOOO", &PyDict_Type, &addresses, &error, &device, &raw_stream, &stream)) return nullptr;
-  Calls* c = reinterpret_cast<Calls*>(type->tp_alloc(type, 0));
-  if (!c) return nullptr;
-  auto keep = [](PyObject*& to, PyObject* x) {
-    Py_INCREF(x);
-    to = x;
-  };
-  keep(c->error, error);
-  keep(c->device, device);
-  keep(c->raw_stream, raw_stream);
-  keep(c->stream, stream);
-  bool ok = true;
-  auto find = [&](auto& to, const char* name) {
-    PyObject* x = ok ? PyDict_GetItemString(addresses, name) : nullptr;
-    void* p = x ? PyLong_AsVoidPtr(x) : nullptr;
-    if (ok && !p) {
-      if (!PyErr_Occurred()) PyErr_Format(PyExc_KeyError, "no address of %s", name);
-      ok = false;
-    }
-    to = reinterpret_cast<std::remove_reference_t<decltype(to)>>(p);
-  };
-  find(c->last_error, "mb_last_error");
+PyMethodDef methods8[] = {
+    MB_METHOD8("mb_fp8_quant", quant,
+               "mb_fp8_quant($self, x, T_cap=None, meta=None, q=None, s=None)\n--\n\n"
+               "x [rows, W] bfloat16 or float32, dense rows -> (q [rows, W] float8_e4m3fn, s [rows, ceil(W/128)] float8_e8m0fnu)."),
+    MB_METHOD8("mb_fp8_dequant", dequant,
+               "mb_fp8_dequant($self, q, s, dtype=None, T_cap=None, meta=None, out=None)\n--\n\n"
+               "8-bit rows -> [rows, W] bfloat16 (or dtype float32)."),
+    MB_METHOD8("mb_fp8_quant_weight", quant_weight,
+               "mb_fp8_quant_weight($self, w, transposed=True, q=None, s=None, qt=None, st=None)\n--\n\n"
+               "w [n_out, n_in] -> (q, s, qt, st): 8-bit values with a scale for each 128 x 128 block, and the same transposed;\n"
+               "(q, s) alone with transposed=False."),
+    MB_METHOD8("mb_linear_fp8_fwd", linear,
+               "mb_linear_fp8_fwd($self, xq, xs, wq, ws, dtype=None, T_cap=None, meta=None, y=None)\n--\n\n"
+               "y = x @ w.T for 8-bit rows x [rows, n_in] and an 8-bit weight w [n_out, n_in]; bfloat16, or dtype float32.\n"
+               "With dy's rows and the transposed weight it is the data gradient."),
+    MB_METHOD8("mb_linear_fp8_wgrad", wgrad,
+               "mb_linear_fp8_wgrad($self, dy, xq, xs, dys=None, T_cap=None, meta=None, dw=None, workspace=None)\n--\n\n"
+               "dw = dy.T @ x, float32, for stored 8-bit rows x [rows, n_in]; dy [rows, n_out] bfloat16, or 8-bit rows with dys."),
+    MB_METHOD8("mb_geglu_fp8_act", geglu_act,
+               "mb_geglu_fp8_act($self, xq, xs, w1vq, w1vs, T_cap=None, meta=None, actq=None, acts=None)\n--\n\n"
+               "GeLU(x W1) * x V for 8-bit rows x and the 8-bit weight [2*inter, hidden] (W1 transposed over V transposed), as\n"
+               "8-bit rows: (actq [rows, inter], acts)."),
+    MB_METHOD8("mb_gelu_gate_fp8_bwd", gate_bwd,
+               "mb_gelu_gate_fp8_bwd($self, da, hg, hgs=None, T_cap=None, meta=None, dhgq=None, dhgs=None)\n--\n\n"
+               "Backward of GeLU(h) * g from da [rows, inter] bfloat16 and h | g [rows, 2*inter] (bfloat16, or 8-bit rows with\n"
+               "hgs), as 8-bit rows dh | dg: (dhgq [rows, 2*inter], dhgs)."),
+    {nullptr, nullptr, 0, nullptr}};
+
+void find_all(Calls* c, const std::function<void(void**, const char*)>& address) {
+  auto find = [&](auto& to, const char* name) { address(reinterpret_cast<void**>(&to), name); };
   find(c->unpad_index, "mb_unpad_index");
   find(c->unpad, "mb_unpad");
   find(c->pad, "mb_pad");
@@ -589,6 +816,46 @@ PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
   find(c->geglu_bwd, "mb_geglu_bwd");
   find(c->geglu_bwd_bytes, "mb_geglu_bwd_workspace_bytes");
   find(c->linear_fwd, "mb_linear_fwd");
+}
+void find_all(Fp8Calls* c, const std::function<void(void**, const char*)>& address) {
+  auto find = [&](auto& to, const char* name) { address(reinterpret_cast<void**>(&to), name); };
+  find(c->quant, "mb_fp8_quant");
+  find(c->dequant, "mb_fp8_dequant");
+  find(c->quant_weight, "mb_fp8_quant_weight");
+  find(c->linear, "mb_linear_fp8_fwd");
+  find(c->wgrad, "mb_linear_fp8_wgrad");
+  find(c->wgrad_bytes, "mb_linear_fp8_wgrad_workspace_bytes");
+  find(c->act, "mb_geglu_fp8_act");
+  find(c->gate_bwd, "mb_gelu_gate_fp8_bwd");
+}
+
+// Calls(addresses, error, device, raw_stream, stream): `addresses` maps names of the C ABI to function addresses.
+template <typename C>
+PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
+  PyObject *addresses, *error, *device, *raw_stream, *stream;
+  if (!PyArg_ParseTuple(args, "O!OOOO", &PyDict_Type, &addresses, &error, &device, &raw_stream, &stream)) return nullptr;
+  C* c = reinterpret_cast<C*>(type->tp_alloc(type, 0));
+  if (!c) return nullptr;
+  auto keep = [](PyObject*& to, PyObject* x) {
+    Py_INCREF(x);
+    to = x;
+  };
+  keep(c->error, error);
+  keep(c->device, device);
+  keep(c->raw_stream, raw_stream);
+  keep(c->stream, stream);
+  bool ok = true;
+  auto address = [&](void** to, const char* name) {
+    PyObject* x = ok ? PyDict_GetItemString(addresses, name) : nullptr;
+    void* p = x ? PyLong_AsVoidPtr(x) : nullptr;
+    if (ok && !p) {
+      if (!PyErr_Occurred()) PyErr_Format(PyExc_KeyError, "no address of %s", name);
+      ok = false;
+    }
+    *to = p;
+  };
+  address(reinterpret_cast<void**>(&c->last_error), "mb_last_error");
+  find_all(c, address);
   if (!ok) {
     Py_DECREF(c);
     return nullptr;
@@ -597,7 +864,7 @@ PyObject* calls_new(PyTypeObject* type, PyObject* args, PyObject*) {
 }
 
 void calls_dealloc(PyObject* self) {
-  Calls* c = reinterpret_cast<Calls*>(self);
+  Host* c = reinterpret_cast<Host*>(self);
   Py_XDECREF(c->error);
   Py_XDECREF(c->device);
   Py_XDECREF(c->raw_stream);
@@ -607,11 +874,16 @@ void calls_dealloc(PyObject* self) {
   Py_DECREF(type);
 }
 
-PyType_Slot slots[] = {{Py_tp_new, (void*)calls_new},
+PyType_Slot slots[] = {{Py_tp_new, (void*)calls_new<Calls>},
                        {Py_tp_dealloc, (void*)calls_dealloc},
                        {Py_tp_methods, methods},
                        {0, nullptr}};
 PyType_Spec spec = {"_mosaic_marshal.Calls", sizeof(Calls), 0, Py_TPFLAGS_DEFAULT, slots};
+PyType_Slot slots8[] = {{Py_tp_new, (void*)calls_new<Fp8Calls>},
+                        {Py_tp_dealloc, (void*)calls_dealloc},
+                        {Py_tp_methods, methods8},
+                        {0, nullptr}};
+PyType_Spec spec8 = {"_mosaic_marshal.Fp8Calls", sizeof(Fp8Calls), 0, Py_TPFLAGS_DEFAULT, slots8};
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_mosaic_marshal", nullptr, 0, nullptr, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
@@ -619,11 +891,13 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_mosaic_marshal", nullptr, 0, 
 extern "C" __attribute__((visibility("default"))) PyObject* PyInit__mosaic_marshal() {
   PyObject* m = PyModule_Create(&module_def);
   if (!m) return nullptr;
-  PyObject* type = PyType_FromSpec(&spec);
-  if (!type || PyModule_AddObject(m, "Calls", type) < 0) {
-    Py_XDECREF(type);
-    Py_DECREF(m);
-    return nullptr;
+  for (auto [name, made] : {std::pair<const char*, PyType_Spec*>{"Calls", &spec}, {"Fp8Calls", &spec8}}) {
+    PyObject* type = PyType_FromSpec(made);
+    if (!type || PyModule_AddObject(m, name, type) < 0) {
+      Py_XDECREF(type);
+      Py_DECREF(m);
+      return nullptr;
+    }
   }
   if (PyModule_AddStringConstant(m, "torch_version", TORCH_VERSION) < 0) {
     Py_DECREF(m);

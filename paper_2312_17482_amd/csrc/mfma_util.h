@@ -110,6 +110,15 @@ __device__ __forceinline__ void load_word_to_lds(uint32_t lds, uint32_t lane_off
                : "memory");
   (void)m0;
 }
+// The same for 64 single bytes: each lands as a word of its own, zero-extended.
+__device__ __forceinline__ void load_byte_to_lds(uint32_t lds, uint32_t lane_off, u32x4 rsrc, uint32_t scalar_off) {
+  uint32_t m0;
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_ubyte %2, %3, %4 offen lds"
+               : "=&{m0}"(m0)
+               : "s"(lds), "v"(lane_off), "s"(rsrc), "s"(scalar_off)
+               : "memory");
+  (void)m0;
+}
 // load_to_lds with a 64-bit address per lane.
 __device__ __forceinline__ void load_to_lds_each(uint32_t lds, const void* lane_ptr) {
   uint32_t m0;
