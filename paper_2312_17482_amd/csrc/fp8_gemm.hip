@@ -76,9 +76,16 @@ constexpr int kLdsBytes = kStages * kStageBytes<kMB, kWN, kNB> + 2 * kWN * 2048;
 
 // Workgroup of 2 kWN waves (2 along the tokens by kWN along the weight rows): tiles blockIdx.x, + gridDim.x, ... of 64 kMB tokens
 // x 32 kWN kNB weight rows; a wave computes 32 kMB x 32 kNB.  Token fragments rotate through kDepth buffers.
+//
+// Stages free up in two halves where that can be had (kTwice: 256 tokens).  A step is eight slots of two matrix instructions, a
+// slot a block of 32 tokens and a half of the step's k; the slots of blocks 0 and 1 come first.  By the middle of the step
+// every wave has read all of the weight and these blocks, and a barrier there lets their places be requested for the step after
+// next; those of blocks 2 and 3 follow at the end.  So everything is requested one and a half steps before it is needed, with
+// two stages: a step's 64 KB take 1.2 to 1.5 us to come when requested at once, its matrix instructions 1.0 us.
 template <int kMode, int kMB, int kWN, int kNB, int kStages, int kDepth>
 __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __restrict__ smem, int wave) {
   constexpr bool kGated = kMode == kAct, kExact = is_exact(kMode);
+  constexpr bool kTwice = kMB == 4 && kWN == 4 && kStages == 2 && kDepth == 2;
   constexpr int kBM = 64 * kMB, kBN = 32 * kWN * kNB, kWaves = 2 * kWN;
   static_assert(!kGated || (kNB == 2 && kBN == 256), "the gate pairs the wave's two weight blocks; 128 columns are a block");
   constexpr int kRows = kBM + kBN;
@@ -148,6 +155,9 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
     }
   };
   constexpr int kFetches = kLoads + 1;
+  // kTwice: loads 1 and 3 bring token blocks 2 and 3 of either half of the waves, the others what is free in the middle.
+  constexpr int kLate = kTwice ? 2 : kFetches;   // loads at the end of a step
+  auto fetch_nth = [&](int n, int stage, int kt) { fetch_one(!kTwice ? n : n < kLate ? 2 * n + 1 : n < 4 ? 2 * n - 4 : n, stage, kt); };
 
   // Fragments: a lane's 32 bytes of half h of a row are pieces 4 h + g and 4 h + 2 + g (which k a byte belongs to does not
   // matter as long as both operands agree).
@@ -160,7 +170,8 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
   constexpr uint32_t kWBlock = (kGated ? kBN / 2 : 32) * kStep;
   i32x8 xf[kDepth], wf[2][kNB];
   bf16x8 wb[kNB][4];   // exact: the half's weight fragments, 8 k each
-  uint32_t sx[kMB], sw[kGated ? 2 : 1], sx_next[kMB], sw_next[kGated ? 2 : 1];
+  constexpr int kSw = kGated ? 2 : 1;
+  uint32_t sx[kMB], sw[kSw], sx_next[kMB], sw_next[kSw];
   auto read32 = [&](int stage, uint32_t place, int half) {
     const uint8_t* p = smem + stage * kStage + place;
     const u32x4 a = *reinterpret_cast<const u32x4*>(p + frag[2 * half]), b = *reinterpret_cast<const u32x4*>(p + frag[2 * half + 1]);
@@ -172,21 +183,22 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
     }
     return r;
   };
-  auto read_x = [&](int stage, int slot) { xf[slot % kDepth] = read32(stage, xrow + (slot % kMB) * 32 * kStep, slot / kMB); };
+  constexpr auto block_of = [](int slot) { return kTwice ? 2 * (slot / 4) + (slot % 4 == 1 || slot % 4 == 2) : slot % kMB; };
+  constexpr auto half_of = [](int slot) { return kTwice ? slot % 4 / 2 : slot / kMB; };
+  auto read_x = [&](int stage, int slot) { xf[slot % kDepth] = read32(stage, xrow + block_of(slot) * 32 * kStep, half_of(slot)); };
   auto read_w = [&](int stage, int half) {
 #pragma unroll
     for (int i = 0; i < kNB; ++i) wf[half][i] = read32(stage, wrow + i * kWBlock, half);
   };
-  auto read_scales = [&](int stage) {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(smem + stage * kStage + kScales);
+  const uint32_t* const scales = reinterpret_cast<const uint32_t*>(smem + kScales);
+  auto read_x_scales = [&](int stage, int from, int to, uint32_t (&sc)[kMB]) {
 #pragma unroll
-    for (int mb = 0; mb < kMB; ++mb) sx_next[mb] = p[wm * 32 * kMB + mb * 32 + c];
-    if (kGated) {
-      sw_next[0] = p[kMB * 64];
-      sw_next[kGated ? 1 : 0] = p[kMB * 64 + 1];
-    } else {
-      sw_next[0] = p[kMB * 64 + (wn * 32 * kNB) / kFp8Block];
-    }
+    for (int mb = from; mb < to; ++mb) sc[mb] = scales[stage * (kStage / 4) + wm * 32 * kMB + mb * 32 + c];
+  };
+  auto read_w_scales = [&](int stage) {
+#pragma unroll
+    for (int i = 0; i < kSw; ++i)
+      sw_next[i] = scales[stage * (kStage / 4) + kMB * 64 + (kGated ? i : (wn * 32 * kNB) / kFp8Block)];
   };
   f32x16 acc[kNB][kMB];
 
@@ -203,20 +215,22 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
 #pragma unroll
   for (int st = 0; st < kStages; ++st) {
 #pragma unroll
-    for (int i = 0; i < kFetches; ++i) fetch_one(i, st, f_kt);
+    for (int i = 0; i < kFetches; ++i) fetch_nth((i + kLate) % kFetches, st, f_kt);   // (the late ones last)
     advance();
   }
-  stage_ready<(kStages - 1) * kFetches>();
+  stage_ready<(kStages - 1) * kFetches + (kTwice ? kLate : 0)>();
 #pragma unroll
   for (int i = 0; i < kDepth - 1; ++i) read_x(0, i);
   read_w(0, 0);
-  read_scales(0);
+  if (kTwice) read_x_scales(0, 0, 2, sx);
+  else read_x_scales(0, 0, kMB, sx_next);
+  read_w_scales(0);
 
   // stores of an epilogue that every wave issues
   constexpr int kStores = kGated ? kMB : (kMode == kF32 ? 4 : 2) * kMB * kNB;
-  constexpr int kNewer = (kStages - 2) * kFetches;
+  constexpr int kNewer = kTwice ? kFetches : (kStages - 2) * kFetches;   // loads newer than what a barrier waits for
   static_assert(kNewer + kStores < 64, "fits the counter");
-  int after_stores = 0;   // whether the newest memory operations but the loads ahead are an epilogue's stores
+  int loose = 0;   // barriers that let the stores of the epilogue before them travel on: what they wait for is older
   int stage = 0;
   for (int tile = blockIdx.x; tile < total; tile += gridDim.x) {
 #pragma unroll
@@ -226,49 +240,70 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[nb][mb][v] = 0.f;
     // A slot is kNB matrix instructions; kDepth - 1 slots ahead its token fragment is read.  In front of slot kSlots - kDepth + 1
-    // stands the barrier behind which nobody reads this stage any more and the next one has arrived.
+    // stands the barrier behind which nobody reads this stage any more and the next one has arrived (kTwice: its weight and
+    // first token blocks; the others behind the barrier in the middle).
 #pragma unroll 1
     for (int kt = 0; kt < nk; ++kt) {
       const int next = stage + 1 == kStages ? 0 : stage + 1;
 #pragma unroll
-      for (int mb = 0; mb < kMB; ++mb) sx[mb] = sx_next[mb];
+      for (int i = 0; i < (kTwice ? 0 : kMB); ++i) sx[i] = sx_next[i];
 #pragma unroll
-      for (int i = 0; i < (kGated ? 2 : 1); ++i) sw[i] = sw_next[i];
+      for (int i = 0; i < kSw; ++i) sw[i] = sw_next[i];
       constexpr int kLast = kSlots - kDepth + 1;   // the first slot behind the barrier
-#pragma unroll
-      for (int i = 0; i < kSlots; ++i) {
-        if (i == kLast) stage_ready_or_stores<kNewer, kStores>(after_stores);
+      constexpr int kMiddle = kTwice ? kSlots / 2 - 1 : -1;
+      // What a slot does beside its products, behind the first of them (whose operands are there): the barrier and the reads
+      // that the next slots wait for, under the matrix cores' work; the loads behind the last one.
+      auto beside = [&](int i) {
+        if (i == kLast || i == kMiddle) {
+          stage_ready_or_stores<kNewer, kStores>(loose);
+          loose -= loose > 0;
+        }
         if (i + kDepth - 1 < kSlots) read_x(stage, i + kDepth - 1);
         else read_x(next, i + kDepth - 1 - kSlots);
+        if (i == kLast) read_w(next, 0);
         if (i == 0) read_w(stage, 1);
+        if (kTwice && i == 1) read_x_scales(stage, 2, 4, sx);   // (in front of the barrier behind which their place is refilled)
         if (i == kLast) {
-          read_w(next, 0);
-          read_scales(next);
+          if (kTwice) read_x_scales(next, 0, 2, sx);
+          else read_x_scales(next, 0, kMB, sx_next);
+          read_w_scales(next);
         }
+      };
+      auto request = [&](int i) {
         if (i >= kLast) {
 #pragma unroll
-          for (int f = i - kLast; f < kFetches; f += kSlots - kLast) fetch_one(f, stage, f_kt);
+          for (int f = i - kLast; f < kLate; f += kSlots - kLast) fetch_nth(f, stage, f_kt);
+        } else if (kTwice && i >= kMiddle) {
+#pragma unroll
+          for (int f = kLate + i - kMiddle; f < kFetches; f += kLast - kMiddle) fetch_nth(f, stage, f_kt);
         }
-        __builtin_amdgcn_sched_barrier(0);
+      };
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) {
+        const int mb = block_of(i), half = half_of(i);
         if constexpr (kExact) {
-          if (i % kMB == 0) {
+          if (i == 0 || half != half_of(i - 1)) {
 #pragma unroll
             for (int nb = 0; nb < kNB; ++nb)
 #pragma unroll
               for (int p = 0; p < 4; ++p)
-                wb[nb][p] = to_bf16x8(wf[i / kMB][nb][2 * p], wf[i / kMB][nb][2 * p + 1], __uint_as_float(sw[kGated ? nb : 0] << 23));
+                wb[nb][p] = to_bf16x8(wf[half][nb][2 * p], wf[half][nb][2 * p + 1], __uint_as_float(sw[kGated ? nb : 0] << 23));
           }
-#pragma unroll
-          for (int p = 0; p < 4; ++p) {
-            const bf16x8 xb = to_bf16x8(xf[i % kDepth][2 * p], xf[i % kDepth][2 * p + 1], __uint_as_float(sx[i % kMB] << 23));
-#pragma unroll
-            for (int nb = 0; nb < kNB; ++nb) acc[nb][i % kMB] = mfma32(wb[nb][p], xb, acc[nb][i % kMB]);
-          }
-        } else {
-#pragma unroll
-          for (int nb = 0; nb < kNB; ++nb)
-            acc[nb][i % kMB] = mfma_scaled(wf[i / kMB][nb], xf[i % kDepth], acc[nb][i % kMB], sw[kGated ? nb : 0], sx[i % kMB]);
         }
+#pragma unroll
+        for (int p = 0; p < (kExact ? 4 : 1); ++p) {
+          bf16x8 xb;
+          if constexpr (kExact) xb = to_bf16x8(xf[i % kDepth][2 * p], xf[i % kDepth][2 * p + 1], __uint_as_float(sx[mb] << 23));
+#pragma unroll
+          for (int nb = 0; nb < kNB; ++nb) {
+            if constexpr (kExact) acc[nb][mb] = mfma32(wb[nb][p], xb, acc[nb][mb]);
+            else acc[nb][mb] = mfma_scaled(wf[half][nb], xf[i % kDepth], acc[nb][mb], sw[kGated ? nb : 0], sx[mb]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (p == 0 && nb == 0) beside(i);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+        request(i);
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
@@ -276,10 +311,9 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
 #pragma unroll
         for (int mb = 0; mb < kMB; ++mb) asm volatile("" : "+v"(acc[nb][mb]));   // (see stage_ready_or_stores)
       advance();
-      after_stores = 0;
       stage = next;
     }
-    after_stores = 1;
+    loose = kTwice ? 3 : 1;
 
     int m0, n0;
     locate(tile, m0, n0);
