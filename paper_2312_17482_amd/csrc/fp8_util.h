@@ -33,6 +33,14 @@ __device__ __forceinline__ float finite_abs(float x) {
 __device__ __forceinline__ int scale_byte(float amax) {
   return max((int)((__float_as_uint(amax) + 0x1fffffu) >> 23) - 8, 1);
 }
+// Whether a largest magnitude lies so near to 448 * 2^e that an error of `reach` 2^-23 of its power of two could decide between
+// two scales, and the least magnitude that does.
+__device__ __forceinline__ bool near_border(float amax, uint32_t reach) {
+  return (__float_as_uint(amax) & 0x7fffffu) - (0x600000u - reach) < 2 * reach;
+}
+__device__ __forceinline__ float border_from(float amax, uint32_t reach) {
+  return __uint_as_float((__float_as_uint(amax) & 0x7f800000u) | (0x600000u - reach));
+}
 // 1 / scale, exact; bytes 1 .. 247.
 __device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 // The scale itself; byte 255 stands for NaN.
@@ -101,6 +109,54 @@ __device__ __forceinline__ void gelu_tail_and_grad(float h, float& val, float& g
   const float cdf = h < 0.f ? u : 1.0f - u;
   val = h * cdf;
   grad = fmaf(h * 0.3989422804014327f, e, cdf);
+}
+// Sum over the wave, without the detour through LDS that a shuffle takes: 16 lanes by data-parallel moves (xor 1, 2, then the
+// mirror images of 8 and 16 lanes), then the row and half-wave swaps.
+template <int kCtrl>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_mov_dpp((int)(uint32_t)u, kCtrl, 0xf, 0xf, true);
+  const uint32_t hi = __builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), kCtrl, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double joined(uint32_t lo, uint32_t hi) { return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo); }
+__device__ __forceinline__ double wave_sum(double x) {
+  x += moved<0xb1>(x);    // quad_perm 1, 0, 3, 2
+  x += moved<0x4e>(x);    // quad_perm 2, 3, 0, 1
+  x += moved<0x141>(x);   // mirrored within 8 lanes
+  x += moved<0x140>(x);   // mirrored within 16 lanes
+  uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const auto a = __builtin_amdgcn_permlane16_swap((uint32_t)u, (uint32_t)u, false, false);
+  const auto b = __builtin_amdgcn_permlane16_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  x = joined(a[0], b[0]) + joined(a[1], b[1]);
+  u = __builtin_bit_cast(uint64_t, x);
+  const auto c = __builtin_amdgcn_permlane32_swap((uint32_t)u, (uint32_t)u, false, false);
+  const auto d = __builtin_amdgcn_permlane32_swap((uint32_t)(u >> 32), (uint32_t)(u >> 32), false, false);
+  return joined(c[0], d[0]) + joined(c[1], d[1]);
+}
+
+// GeLU in 64 bits: normal_tail's form with t = 1 / (1 + 0.3 x) and P of degree 10 (4e-10 of the value), to decide between scales.
+__device__ __forceinline__ double gelu64(double h) {
+  const double x = fabs(h) * 0.70710678118654752440, t = 1.0 / fma(0.3, x, 1.0);
+  double p = 0.055734015794935123;
+  p = fma(p, t, -0.33301687949411679);
+  p = fma(p, t, 0.74512765630325928);
+  p = fma(p, t, -0.84218931949770892);
+  p = fma(p, t, 0.77589148990779011);
+  p = fma(p, t, -0.28565462890504778);
+  p = fma(p, t, 0.26894751688341517);
+  p = fma(p, t, 0.10941256579431252);
+  p = fma(p, t, 0.16781163040879243);
+  p = fma(p, t, 0.16865276238932064);
+  p = fma(p, t, 0.16928319008836501);
+  const double tail = 0.5 * p * t * exp(-x * x);
+  return h * (h < 0.0 ? tail : 1.0 - tail);
+}
+// A value as a float that lies on the same side of the scales' borders, 448 * 2^e, which belong to the smaller one.
+__device__ __forceinline__ float round_beside_border(double v) {
+  const float f = (float)v;
+  const uint32_t bits = __float_as_uint(f);
+  return (bits & 0x7fffffu) == 0x600000u && fabs(v) > (double)fabsf(f) ? __uint_as_float(bits + 1) : f;
 }
 
 }  // namespace mb

@@ -278,6 +278,41 @@ def test_act_far_negative_gates_keep_their_digits():
     check_eight(q, s, v, 2e-5 * np.abs(v))
 
 
+def act_case(seed, T, hidden, inter):
+    rng = np.random.default_rng(seed)
+    x = rng.standard_normal((T, hidden)) * np.where(rng.random(hidden) < 0.02, 12.0, 1.0)
+    x, xq, xs = stored(x)
+    w, wq, ws = stored(rng.standard_normal((2 * inter, hidden)) * 0.03, 128)
+    hg = x @ w.T
+    return orc.gelu(hg[:, :inter])[0] * hg[:, inter:], (xq, xs, wq, ws)
+
+
+def test_act_scales_are_the_definitions():
+    """Where the products' own grouping of their sums (some 1e-5 of a value) would decide: 48,000 blocks, of which it moves a few
+    across the border between two scales."""
+    v, args = act_case(31, 6000, 768, 1024)
+    top = np.abs(v).reshape(6000, 8, 128).max(2)
+    beside = np.ldexp(448.0, np.floor(np.log2(top / 448.0) + 0.5).astype(int))
+    clear = np.abs(top / beside - 1) > 1e-8
+    assert clear.sum() > 47990 and (np.abs(top / beside - 1) < 3e-5).sum() >= 2
+    _, s = mb.mb_geglu_fp8_act(*args)
+    assert np.array_equal(exps(s)[clear], orc.scale_exponents(v)[clear])
+
+
+def test_act_of_equal_rows_on_a_border():
+    """Every token of a batch at the border at once: what is decided one by one comes to an end, and all decide alike."""
+    T, hidden, inter = 700, 128, 256
+    x, w = np.zeros((T, hidden)), np.zeros((2 * inter, hidden))
+    x[:, 0], x[:, 1] = 16.0, 1.0
+    w[:inter, 0], w[:inter, 1] = 1.0, 2.0 ** -13                  # h = 16 + 2^-13, GeLU(h) = h
+    w[inter:, 0] = 1.75                                           # v = 448 (1 + 2^-17)
+    (xv, xq, xs), (wv, wq, ws) = stored(x), stored(w, 128)
+    h = xv @ wv[:inter].T
+    q, s = mb.mb_geglu_fp8_act(xq, xs, wq, ws)
+    want = orc.scale_exponents(orc.gelu(h)[0] * (xv @ wv[inter:].T))
+    assert np.all(exps(s) == want) and np.all(np.abs(val(q) * np.ldexp(1.0, want[0, 0]) / 448 - 1) <= 2.0 ** -4)
+
+
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("T,inter", [(1, 128), (5, 256), (33, 128), (300, 640)])
 def test_gate_backward(T, inter, eight):
