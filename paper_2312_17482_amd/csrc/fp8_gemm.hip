@@ -495,6 +495,119 @@ __global__ __launch_bounds__(128 * kWN, kWN / 2) void fp8_gemm_kernel(Product pr
   fp8_tiles<kMode, kMB, kWN, kNB, kStages, kDepth>(pr, T, smem, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
+// Products of few rows, whose time is that of the way to memory and back: 16 kA tokens x 16 kB columns by 8 waves that share the
+// contraction, wave w its blocks w, w + 8, ... of 128 k.  No stages and no barrier in it: a wave requests a block's rows straight
+// into the registers the matrix instruction reads (v_mfma_scale_f32_16x16x128_f8f6f4, one a block; exact: four of
+// v_mfma_f32_16x16x32_bf16), the next block's while it multiplies, and the waves' sums meet in LDS once, added in order.
+constexpr int kSliceWaves = 8;
+template <int kMode, int kA, int kB>
+__global__ __launch_bounds__(64 * kSliceWaves) void fp8_slice_kernel(Product pr) {
+  constexpr bool kExact = is_exact(kMode);
+  constexpr int kTM = 16 * kA, kTN = 16 * kB, kPieces = kTN / 4;   // 16-byte pieces of a token's sums
+  __shared__ __attribute__((aligned(16))) float sums[kSliceWaves * kTM * kTN];
+  const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
+  const int m0 = blockIdx.y * kTM, n0 = blockIdx.x * kTN;
+  if (m0 >= T) return;
+  const int K = pr.K, blocks = fp8_blocks(K), w_rows = pr.w_rows;
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int xrows = min(T - m0, kTM), wrows = min(w_rows - n0, kTN);
+  const __amdgpu_buffer_rsrc_t xr = uniform_rsrc(pr.x + (int64_t)m0 * K, (uint32_t)xrows * (uint32_t)K);
+  const __amdgpu_buffer_rsrc_t wr = uniform_rsrc(pr.w + (int64_t)n0 * K, (uint32_t)wrows * (uint32_t)K);
+  const __amdgpu_buffer_rsrc_t xsr = uniform_rsrc(pr.xs + (int64_t)m0 * blocks, (uint32_t)xrows * (uint32_t)blocks);
+  const __amdgpu_buffer_rsrc_t wsr = uniform_rsrc(pr.ws, (uint32_t)fp8_blocks(w_rows) * (uint32_t)blocks);
+  // A lane's 32 bytes of a row: pieces g and g + 4 (four lanes request 64 bytes in one go).  Rows and pieces that do not
+  // exist are out of the descriptor's range and zeros.
+  struct Block {
+    i32x8 x[kA], w[kB];
+    uint32_t xs[kA], ws[kB];
+  };
+  auto request = [&](Block& b, int kb) {
+    auto rows = [&](i32x8& r, __amdgpu_buffer_rsrc_t from, int row) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int k = kb * kFp8Block + (g + 4 * u) * 16;
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, k < K ? (uint32_t)row * (uint32_t)K + k : 0x80000000u, 0, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[4 * u + i] = (int)v[i];
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < kB; ++i) rows(b.w[i], wr, 16 * i + c);
+#pragma unroll
+    for (int i = 0; i < kA; ++i) rows(b.x[i], xr, 16 * i + c);
+#pragma unroll
+    for (int i = 0; i < kB; ++i)
+      b.ws[i] = __builtin_amdgcn_raw_buffer_load_b8(wsr, (uint32_t)((n0 + 16 * i) / kFp8Block) * (uint32_t)blocks + kb, 0, 0);
+#pragma unroll
+    for (int i = 0; i < kA; ++i) b.xs[i] = __builtin_amdgcn_raw_buffer_load_b8(xsr, (uint32_t)(16 * i + c) * (uint32_t)blocks + kb, 0, 0);
+  };
+  f32x4 acc[kA][kB] = {};
+  auto multiply = [&](const Block& b) {
+    if constexpr (kExact) {
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        bf16x8 xb[kA];
+#pragma unroll
+        for (int i = 0; i < kA; ++i) xb[i] = to_bf16x8(b.x[i][2 * p], b.x[i][2 * p + 1], __uint_as_float(b.xs[i] << 23));
+#pragma unroll
+        for (int j = 0; j < kB; ++j) {
+          const bf16x8 wb = to_bf16x8(b.w[j][2 * p], b.w[j][2 * p + 1], __uint_as_float(b.ws[j] << 23));
+#pragma unroll
+          for (int i = 0; i < kA; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[i], acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kB; ++j)
+#pragma unroll
+        for (int i = 0; i < kA; ++i)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.w[j], b.x[i], acc[i][j], 0, 0, 0, (int)b.ws[j], 0, (int)b.xs[i]);
+    }
+  };
+  Block now, ahead;
+  if (wave < blocks) request(now, wave);
+  for (int kb = wave; kb < blocks; kb += 2 * kSliceWaves) {
+    if (kb + kSliceWaves < blocks) request(ahead, kb + kSliceWaves);
+    multiply(now);
+    if (kb + kSliceWaves >= blocks) break;
+    if (kb + 2 * kSliceWaves < blocks) request(now, kb + 2 * kSliceWaves);
+    multiply(ahead);
+  }
+  // Lane (c, g) holds columns 16 j + 4 g .. + 3 of token 16 i + c: piece 4 j + g of the token's row (at place ^ token, so that
+  // the 16 tokens' pieces lie in different banks).
+  auto place = [](int t, int p) { return (t * kPieces + (p ^ (t & (kPieces - 1)))) * 4; };
+  if (wave < blocks) {
+#pragma unroll
+    for (int i = 0; i < kA; ++i)
+#pragma unroll
+      for (int j = 0; j < kB; ++j)
+        *reinterpret_cast<f32x4*>(&sums[wave * kTM * kTN + place(16 * i + c, 4 * j + g)]) = acc[i][j];
+  }
+  __syncthreads();
+  const int waves = min(blocks, kSliceWaves);
+  constexpr int kEs = kMode == kF32 ? 4 : 2;
+  uint8_t* const out = static_cast<uint8_t*>(pr.out);
+  for (int at = tid; at < kTM * kPieces; at += 64 * kSliceWaves) {
+    const int t = at / kPieces, p = at % kPieces, col = n0 + 4 * p;
+    if (m0 + t >= T || col >= w_rows) continue;
+    f32x4 v = *reinterpret_cast<const f32x4*>(&sums[place(t, p)]);
+    for (int i = 1; i < waves; ++i) v += *reinterpret_cast<const f32x4*>(&sums[i * kTM * kTN + place(t, p)]);
+    uint8_t* const to = out + ((int64_t)(m0 + t) * pr.ldo + col) * kEs;
+    if constexpr (kMode == kF32) {
+      *reinterpret_cast<f32x4*>(to) = v;
+    } else {
+      *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    }
+  }
+}
+
+template <int kMode, int kA, int kB>
+void launch_slices(const Product& pr, hipStream_t stream) {
+  const dim3 grid((pr.w_rows + 16 * kB - 1) / (16 * kB), (pr.T_cap + 16 * kA - 1) / (16 * kA));
+  fp8_slice_kernel<kMode, kA, kB><<<grid, dim3(64 * kSliceWaves), 0, stream>>>(pr);
+}
+
 template <int kMode, int kMB, int kWN, int kNB, int kStages, int kDepth>
 void launch_tiles(Product pr, int cols, hipStream_t stream) {
   constexpr int kBN = 32 * kWN * kNB;
@@ -504,10 +617,60 @@ void launch_tiles(Product pr, int cols, hipStream_t stream) {
       <<<dim3((unsigned)(total < kComputeUnits ? total : kComputeUnits)), dim3(128 * kWN), 0, stream>>>(pr);
 }
 
+// Estimated microseconds in tiles of 64 `mb` tokens: rounds over the compute units, a step and a tile's start and end each.
+// (Fitted to 20 shapes of 945 to 32768 tokens, which it meets within a fifth, such as, 64 / 128 / 192 / 256 tokens:
+// 945 x 768 x 2304 7.7 / 9.4 / 11.2 / 11.6 us, 8000 x 768 x 2304 24.4 / 24.0 / 21.4 / 23.8, 26963 x 3072 x 768 80 / 75 / 63 / 66,
+// 32768 x 4096 x 4096 - / 615 / 516 / 442; the activation 945 x 768 x 2 x 3072 16.9 / 14.5 / 17.7 / 19.7.)
+template <int kMode>
+double tile_cost(int T, int cols, int K, int mb) {
+  constexpr double step[5] = {0, 0.55, 0.92, 1.2, 1.4}, ends[5] = {0, 1.2, 2.0, 2.2, 2.5}, gate[5] = {0, 1.0, 1.4, 3.1, 5.3};
+  const int64_t tiles = ((int64_t)T + 64 * mb - 1) / (64 * mb) * ((cols + 255) / 256);
+  const double product = step[mb] * (is_exact(kMode) ? 1.6 : 1.0) * fp8_blocks(K) + ends[mb] + (kMode == kAct ? gate[mb] : 0.0);
+  return 3.5 + (double)((tiles + kComputeUnits - 1) / kComputeUnits) * product;
+}
+// The same in slices of 16 a tokens x 16 b columns, which come at 30 KB a microsecond and compute unit.  (1 x 1024 x 4096 in
+// slices of 1 x 1: 3.4 us, in 64 x 256 tiles 7.6; 64 x 4096 x 1024: 1 x 1 7.3, 2 x 2 11.5, tiles 19.5; 300 x 768 x 768: 2 x 2 4.2, 1 x 1
+// 5.6, tiles 6.9; 945 x 768 x 768: 4 x 4 6.2, 2 x 2 7.6, tiles 7.0; 945 x 768 x 2304: 4 x 4 15.0, tiles 7.7.)
+double slice_cost(int T, int cols, int K, int a, int b) {
+  const int64_t groups = ((int64_t)T + 16 * a - 1) / (16 * a) * ((cols + 16 * b - 1) / (16 * b));
+  return 2.2 + (double)((groups + kComputeUnits - 1) / kComputeUnits) * (16.0 * (a + b) * K / 30e3);
+}
+
+// The way with the least estimate, by the sizes alone.
 template <int kMode>
 void launch_product(const Product& pr, int cols, hipStream_t stream) {
-  if (pr.T_cap <= 128) launch_tiles<kMode, 1, 4, 2, 2, 2>(pr, cols, stream);
-  else launch_tiles<kMode, is_exact(kMode) ? 3 : 4, 4, 2, 2, 2>(pr, cols, stream);
+  const int T = pr.T_cap, K = pr.K;
+  int best = 0;
+  double least = 1e300;
+  auto offer = [&](int id, double cost) {
+    if (cost < least) {
+      least = cost;
+      best = id;
+    }
+  };
+  for (int mb = 1; mb <= (is_exact(kMode) ? 3 : 4); ++mb) offer(mb, tile_cost<kMode>(T, cols, K, mb));
+  if constexpr (kMode != kAct) {
+    if (T <= 4096) {   // (a grid has 65535 rows of workgroups at most; never the least beyond)
+      offer(11, slice_cost(T, cols, K, 1, 1));
+      offer(22, slice_cost(T, cols, K, 2, 2));
+      offer(24, slice_cost(T, cols, K, 2, 4));
+      offer(44, slice_cost(T, cols, K, 4, 4));
+    }
+    switch (best) {
+      case 11: return launch_slices<kMode, 1, 1>(pr, stream);
+      case 22: return launch_slices<kMode, 2, 2>(pr, stream);
+      case 24: return launch_slices<kMode, 2, 4>(pr, stream);
+      case 44: return launch_slices<kMode, 4, 4>(pr, stream);
+      default: break;
+    }
+  }
+  switch (best) {
+    case 1: return launch_tiles<kMode, 1, 4, 2, 3, 2>(pr, cols, stream);
+    case 2: return launch_tiles<kMode, 2, 4, 2, 2, 2>(pr, cols, stream);
+    case 3: return launch_tiles<kMode, 3, 4, 2, 2, 2>(pr, cols, stream);
+    default:
+      if constexpr (!is_exact(kMode)) launch_tiles<kMode, 4, 4, 2, 2, 2>(pr, cols, stream);
+  }
 }
 
 }  // namespace

@@ -10,6 +10,7 @@ namespace mb {
 
 constexpr int kFp8Block = 128;
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __host__ __device__ inline int fp8_blocks(int width) { return (width + kFp8Block - 1) / kFp8Block; }
 
