@@ -39,17 +39,10 @@ __device__ __forceinline__ void store16(uint16_t* p, const float (&x)[16]) {
     *reinterpret_cast<u32x4*>(p + 8 * i) = v;
   }
 }
-__device__ __forceinline__ float largest16(const float (&x)[16]) {
-  float a = 0.f;
-#pragma unroll
-  for (int i = 0; i < 16; ++i) a = fmaxf(a, finite_abs(x[i]));
-  return a;
-}
-__device__ __forceinline__ u32x4 pack16(const float (&x)[16], float inverse) {
+__device__ __forceinline__ u32x4 pack16(const float (&x)[16], int byte) {
   u32x4 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r[i] = pack_e4m3(x[4 * i] * inverse, x[4 * i + 1] * inverse, x[4 * i + 2] * inverse, x[4 * i + 3] * inverse);
+  for (int i = 0; i < 4; ++i) r[i] = pack_e4m3(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3], scale_bits(byte));
   return r;
 }
 
@@ -71,8 +64,8 @@ __global__ __launch_bounds__(256) void fp8_quant_kernel(const T* __restrict__ x,
 #pragma unroll
       for (int i = 0; i < 16; ++i) v[i] = 0.f;
     }
-    const int byte = scale_byte(max_of_8_lanes(largest16(v)));
-    if (col < W) *reinterpret_cast<u32x4*>(q + row * W + col) = pack16(v, scale_inverse(byte));
+    const int byte = scale_byte(max_of_8_lanes(largest_of_16(v)));
+    if (col < W) *reinterpret_cast<u32x4*>(q + row * W + col) = pack16(v, byte);
     if (piece == 0) s[at] = (uint8_t)byte;
   }
 }
@@ -89,14 +82,14 @@ __global__ __launch_bounds__(256) void fp8_dequant_kernel(const uint8_t* __restr
     const int64_t row = at / pieces;
     const int col = (int)(at - row * pieces) * 16;
     const u32x4 w = *reinterpret_cast<const u32x4*>(q + row * W + col);
-    const float scale = scale_value(s[row * blocks + (col >> 7)]);
+    const float scale = scale_bits(s[row * blocks + (col >> 7)]);
     float v[16];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float f[4];
-      unpack_e4m3(w[i], f);
+      unpack_e4m3(w[i], scale, f);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * i + j] = f[j] * scale;
+      for (int j = 0; j < 4; ++j) v[4 * i + j] = f[j];
     }
     store16(x + row * stride + col, v);
   }
@@ -124,17 +117,16 @@ __global__ __launch_bounds__(256) void fp8_quant_weight_kernel(const T* __restri
     }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) a = fmaxf(a, largest16(v[i]));
+  for (int i = 0; i < 4; ++i) a = fmaxf(a, largest_of_16(v[i]));
 #pragma unroll
   for (int k = 1; k < 64; k *= 2) a = fmaxf(a, __shfl_xor(a, k));
   if ((tid & 63) == 0) top[tid >> 6] = a;
   __syncthreads();
   const int byte = scale_byte(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])));
-  const float inverse = scale_inverse(byte);
   u32x4 r[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    r[i] = pack16(v[i], inverse);
+    r[i] = pack16(v[i], byte);
     if (row + i < n_out && col < n_in) *reinterpret_cast<u32x4*>(q + (int64_t)(row + i) * n_in + col) = r[i];
   }
   if (tid == 0) {
@@ -160,8 +152,11 @@ __global__ __launch_bounds__(256) void fp8_quant_weight_kernel(const T* __restri
   }
 }
 
+__device__ __forceinline__ double bf16_value(uint16_t b) { return (double)__uint_as_float((uint32_t)b << 16); }
+
 // Backward of the gate act = GeLU(h) (*) g from dA and h | g (bf16, or 8 bits with scales): dh | dg in 8 bits.  Eight lanes
 // per 128 columns, 16 values of dA, h and g each; both results' blocks are those lanes' own.
+constexpr uint32_t kReach = 1024;   // 7e-5 of a value, twice what normal_tail leaves
 template <bool kEight>
 __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __restrict__ da, const void* __restrict__ hg,
                                                            const uint8_t* __restrict__ hgs, int T_cap,
@@ -181,16 +176,16 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
       const uint8_t* p = static_cast<const uint8_t*>(hg) + place;
       const u32x4 hw = *reinterpret_cast<const u32x4*>(p), gw = *reinterpret_cast<const u32x4*>(p + inter);
       const uint8_t* sc = hgs + row * (2 * blocks) + block;
-      const float hs = scale_value(sc[0]), gs = scale_value(sc[blocks]);
+      const float hs = scale_bits(sc[0]), gs = scale_bits(sc[blocks]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float f[4], e[4];
-        unpack_e4m3(hw[i], f);
-        unpack_e4m3(gw[i], e);
+        unpack_e4m3(hw[i], hs, f);
+        unpack_e4m3(gw[i], gs, e);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          h[4 * i + j] = f[j] * hs;
-          g[4 * i + j] = e[j] * gs;
+          h[4 * i + j] = f[j];
+          g[4 * i + j] = e[j];
         }
       }
     } else {
@@ -205,9 +200,36 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
       h[i] = a[i] * g[i] * grad;
       g[i] = a[i] * val;
     }
-    const int hb = scale_byte(max_of_8_lanes(largest16(h))), gb = scale_byte(max_of_8_lanes(largest16(g)));
-    *reinterpret_cast<u32x4*>(q + place) = pack16(h, scale_inverse(hb));
-    *reinterpret_cast<u32x4*>(q + place + inter) = pack16(g, scale_inverse(gb));
+    float htop = max_of_8_lanes(largest_of_16(h)), gtop = max_of_8_lanes(largest_of_16(g));
+    if (__builtin_expect(__ballot(near_border(htop, kReach) || near_border(gtop, kReach)) != 0, 0)) {
+      // a block in some thousand: its largest values once more, in 64 bits
+      float h64 = 0.f, g64 = 0.f;
+#pragma unroll 1
+      for (int i = 0; i < 16; ++i) {
+        const double x = bf16_value(da[row * inter + col + i]);
+        double hv, gv, slope;
+        if (kEight) {
+          const uint8_t* p = static_cast<const uint8_t*>(hg) + place + i;
+          const uint8_t* sc = hgs + row * (2 * blocks) + block;
+          hv = (double)__builtin_amdgcn_cvt_f32_fp8(p[0], 0) * scale_value(sc[0]);
+          gv = (double)__builtin_amdgcn_cvt_f32_fp8(p[inter], 0) * scale_value(sc[blocks]);
+        } else {
+          const uint16_t* p = static_cast<const uint16_t*>(hg) + place + i;
+          hv = bf16_value(p[0]);
+          gv = bf16_value(p[inter]);
+        }
+        const double value = gelu64(hv, &slope);
+        h64 = fmaxf(h64, finite_abs(round_beside_border(x * gv * slope)));
+        g64 = fmaxf(g64, finite_abs(round_beside_border(x * value)));
+      }
+      h64 = max_of_8_lanes(h64);
+      g64 = max_of_8_lanes(g64);
+      if (near_border(htop, kReach)) htop = h64;
+      if (near_border(gtop, kReach)) gtop = g64;
+    }
+    const int hb = scale_byte(htop), gb = scale_byte(gtop);
+    *reinterpret_cast<u32x4*>(q + place) = pack16(h, hb);
+    *reinterpret_cast<u32x4*>(q + place + inter) = pack16(g, gb);
     if (piece == 0) {
       s[row * (2 * blocks) + block] = (uint8_t)hb;
       s[row * (2 * blocks) + blocks + block] = (uint8_t)gb;

@@ -42,21 +42,32 @@ __device__ __forceinline__ bool near_border(float amax, uint32_t reach) {
 __device__ __forceinline__ float border_from(float amax, uint32_t reach) {
   return __uint_as_float((__float_as_uint(amax) & 0x7f800000u) | (0x600000u - reach));
 }
-// 1 / scale, exact; bytes 1 .. 247.
-__device__ __forceinline__ float scale_inverse(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 // The scale itself; byte 255 stands for NaN.
 __device__ __forceinline__ float scale_value(int byte) {
   return byte == 0 ? __uint_as_float(0x00400000u) : byte == 255 ? __uint_as_float(0x7fc00000u) : __uint_as_float((uint32_t)byte << 23);
 }
 
-// Four values, already divided by their scale, as e4m3 (round to nearest even; what is not finite becomes NaN).
-__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+// Four values as e4m3 under a scale (round to nearest even; what is not finite becomes NaN).  Of `scale` the instruction takes
+// the exponent: byte << 23 as a float.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d, float scale) {
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  s16x2 r = {0, 0};
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+  r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, r);
 }
+__device__ __forceinline__ float scale_bits(int byte) { return __uint_as_float((uint32_t)byte << 23); }
 // Four e4m3 values.
 __device__ __forceinline__ void unpack_e4m3(uint32_t w, float (&x)[4]) {
   const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+  x[0] = lo[0];
+  x[1] = lo[1];
+  x[2] = hi[0];
+  x[3] = hi[1];
+}
+// The same times a scale (its exponent, byte << 23 as a float).
+__device__ __forceinline__ void unpack_e4m3(uint32_t w, float scale, float (&x)[4]) {
+  const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, scale, true);
   x[0] = lo[0];
   x[1] = lo[1];
   x[2] = hi[0];
@@ -82,35 +93,47 @@ __device__ __forceinline__ float max_of_8_lanes(float x) {
 }
 
 // Phi(-|h|) and exp(-h^2 / 2) for the GeLU, Phi the normal distribution function.  With x = |h| / sqrt 2:
-//   Phi(-|h|) = erfc(x) / 2 = t P(t) exp(-x^2) / 2,  t = 1 / (1 + 0.38 x),
-// P of degree 6 through erfc(x) exp(x^2) / t, fitted for the least RELATIVE error over x = 0 .. 9.5 (1.0e-6; 3e-6 with fp32
-// arithmetic up to |h| = 6, 7e-6 up to 12).  Relative, because a block whose gates are all far negative gets a scale of its own: there an
-// absolute error of 1e-7, enough for a bf16 result next to larger ones, would be most of the value.
+//   Phi(-|h|) = erfc(x) / 2 = t P(t) exp(-x^2) / 2,  t = 1 / (1 + 0.53 x),
+// P of degree 4 through erfc(x) exp(x^2) / t, fitted for the least RELATIVE error over x = 0 .. 9.5 (2.9e-5).  Relative, because a
+// block whose gates are all far negative gets a scale of its own: there an absolute error of 1e-7, enough for a bf16 result next
+// to larger ones, would be most of the value.  A stored result is rounded by 2^-4 of itself; where 2.9e-5 could decide the
+// block's scale, 64 bits do.
 __device__ __forceinline__ float normal_tail(float h, float& e) {
-  const float ah = fabsf(h);
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.38f * 0.70710678118654752f, ah, 1.0f));
-  float p = fmaf(0.5f * -0.1250446775797289f, t, 0.5f * 0.3346000856655536f);
-  p = fmaf(p, t, 0.5f * -0.0676826123937758f);
-  p = fmaf(p, t, 0.5f * 0.2460534679856757f);
-  p = fmaf(p, t, 0.5f * 0.1813618473996311f);
-  p = fmaf(p, t, 0.5f * 0.2164089138960925f);
-  p = fmaf(p, t, 0.5f * 0.2143019639678111f);
-  e = __builtin_amdgcn_exp2f(h * h * (-0.5f * kLog2e));
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.53f * 0.70710678118654752f, fabsf(h), 1.0f));
+  float p = fmaf(0.5f * -0.1819639537601447f, t, 0.5f * 0.4030186555514750f);
+  p = fmaf(p, t, 0.5f * 0.1652416641586280f);
+  p = fmaf(p, t, 0.5f * 0.3158106802747941f);
+  p = fmaf(p, t, 0.5f * 0.2978819081133195f);
+  e = __builtin_amdgcn_exp2f(h * (h * (-0.5f * kLog2e)));
   return p * t * e;
 }
-// GeLU(h) = h Phi(h), and its derivative Phi(h) + h phi(h).
+// GeLU(h) = h Phi(h) = max(h, 0) - |h| Phi(-|h|), and with its derivative Phi(h) + h phi(h).
 __device__ __forceinline__ float gelu_tail(float h) {
   float e;
   const float u = normal_tail(h, e);
-  return h * (h < 0.f ? u : 1.0f - u);
+  return fmaf(-fabsf(h), u, fmaxf(h, 0.0f));
 }
 __device__ __forceinline__ void gelu_tail_and_grad(float h, float& val, float& grad) {
   float e;
   const float u = normal_tail(h, e);
+  val = fmaf(-fabsf(h), u, fmaxf(h, 0.0f));
   const float cdf = h < 0.f ? u : 1.0f - u;
-  val = h * cdf;
   grad = fmaf(h * 0.3989422804014327f, e, cdf);
 }
+// Largest finite magnitude of 16 values.
+template <typename V>
+__device__ __forceinline__ float largest_of_16(const V& v) {
+  float a = 0.f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) a = fmaxf(a, fabsf(v[i]));   // (a NaN is passed over)
+  if (__builtin_expect(__ballot(!(a < __builtin_inff())) != 0, 0)) {
+    a = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a = fmaxf(a, finite_abs(v[i]));
+  }
+  return a;
+}
+
 // Sum over the wave, without the detour through LDS that a shuffle takes: 16 lanes by data-parallel moves (xor 1, 2, then the
 // mirror images of 8 and 16 lanes), then the row and half-wave swaps.
 template <int kCtrl>
@@ -136,8 +159,8 @@ __device__ __forceinline__ double wave_sum(double x) {
   return joined(c[0], d[0]) + joined(c[1], d[1]);
 }
 
-// GeLU in 64 bits: normal_tail's form with t = 1 / (1 + 0.3 x) and P of degree 10 (4e-10 of the value), to decide between scales.
-__device__ __forceinline__ double gelu64(double h) {
+// GeLU in 64 bits, and its derivative: normal_tail's form with t = 1 / (1 + 0.3 x) and P of degree 10 (4e-10 of the value), to decide between scales.
+__device__ __forceinline__ double gelu64(double h, double* grad = nullptr) {
   const double x = fabs(h) * 0.70710678118654752440, t = 1.0 / fma(0.3, x, 1.0);
   double p = 0.055734015794935123;
   p = fma(p, t, -0.33301687949411679);
@@ -150,8 +173,9 @@ __device__ __forceinline__ double gelu64(double h) {
   p = fma(p, t, 0.16781163040879243);
   p = fma(p, t, 0.16865276238932064);
   p = fma(p, t, 0.16928319008836501);
-  const double tail = 0.5 * p * t * exp(-x * x);
-  return h * (h < 0.0 ? tail : 1.0 - tail);
+  const double e = exp(-x * x), tail = 0.5 * p * t * e, cdf = h < 0.0 ? tail : 1.0 - tail;
+  if (grad) *grad = cdf + h * 0.39894228040143267794 * e;
+  return h * cdf;
 }
 // A value as a float that lies on the same side of the scales' borders, 448 * 2^e, which belong to the smaller one.
 __device__ __forceinline__ float round_beside_border(double v) {
