@@ -68,13 +68,6 @@ struct Product {
   uint8_t* out_s;                   // kAct: scales [T, gate_row / 128]
 };
 
-// The lane's number, counted afresh: what only rare code needs is not kept in registers for it.
-__device__ __forceinline__ int lane_again() {
-  uint32_t all = ~0u;
-  asm volatile("" : "+s"(all));
-  return __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
-}
-
 // One value GeLU(x W1) (*) x V in 64 bits, by a whole wave: token `row`, column `col`.
 __device__ __forceinline__ double gated_value64(const Product& pr, int row, int col, int lane) {
   const int K = pr.K, blocks = fp8_blocks(K);

@@ -85,6 +85,13 @@ __device__ __forceinline__ bf16x8 to_bf16x8(uint32_t lo, uint32_t hi, float scal
   return as_bf16x8(r);
 }
 
+// The lane's number, counted afresh: what only rare code needs is not kept in registers for it.
+__device__ __forceinline__ int lane_again() {
+  uint32_t all = ~0u;
+  asm volatile("" : "+s"(all));
+  return __builtin_amdgcn_mbcnt_hi(all, __builtin_amdgcn_mbcnt_lo(all, 0u));
+}
+
 // Largest of a value over groups of 8 consecutive lanes (the 8 lanes that hold a block of a row, 16 values each).
 __device__ __forceinline__ float max_of_8_lanes(float x) {
   x = fmaxf(x, __shfl_xor(x, 1));

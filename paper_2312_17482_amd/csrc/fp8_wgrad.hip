@@ -25,8 +25,12 @@ struct Wgrad {
   float* out;                     // of the first split; split s is n_out n_in floats further on, s times
 };
 
-// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.  Piece x (8 bf16 columns) of row r
-// sits at position x ^ 4 (r % 4): the four rows a transposing read touches lie in different banks.
+// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4): the four rows a transposing read touches lie in different
+// banks.  The second 16 pieces of a row lie with even and odd ones exchanged: 16 lanes, each with two pieces of one row from
+// its 16 bytes in 8 bits, write the first of them to different banks so, and then the second.
+__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ (x >> 4 & 1); }
+
+// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.
 template <bool kEight, int kCols>
 struct Stager {
   static constexpr int kPerRow = kCols / (kEight ? 16 : 8);   // 16-byte pieces of a row in memory
@@ -67,17 +71,13 @@ struct Stager {
         byte[i] = __builtin_amdgcn_raw_buffer_load_b8(q, soff, (uint32_t)(i * (512 / kPerRow)) * (uint32_t)blocks, 0);
     }
   }
-  // brings the i-th of what was requested to LDS
+  // brings the i-th 16 bytes of bf16 of what was requested to LDS
+  static constexpr int kParts = kEight ? 2 : 1, kPuts = kN * kParts;
   __device__ __forceinline__ void put(uint16_t* to, int i) const {
-    const int r = row + i * (512 / kPerRow);
-    uint16_t* const at = to + r * kCols;
-    if (kEight) {
-      const float scale = __uint_as_float((uint32_t)byte[i] << 23);
-      *reinterpret_cast<bf16x8*>(at + ((2 * piece) ^ (4 * (r & 3))) * 8) = to_bf16x8(data[i][0], data[i][1], scale);
-      *reinterpret_cast<bf16x8*>(at + ((2 * piece + 1) ^ (4 * (r & 3))) * 8) = to_bf16x8(data[i][2], data[i][3], scale);
-    } else {
-      *reinterpret_cast<u32x4*>(at + (piece ^ (4 * (r & 3))) * 8) = data[i];
-    }
+    const int n = i / kParts, part = i % kParts, r = row + n * (512 / kPerRow);
+    uint16_t* const at = to + r * kCols + place_of(kParts * piece + part, r) * 8;
+    if (kEight) *reinterpret_cast<bf16x8*>(at) = to_bf16x8(data[n][2 * part], data[n][2 * part + 1], scale_bits(byte[n]));
+    else *reinterpret_cast<u32x4*>(at) = data[n];
   }
 };
 
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
 #pragma unroll
   for (int i = 0; i < kFrags; ++i) {
     const int x = (i < kMB ? 4 * (kMB * wm + i) : 8 * wn + 4 * (i - kMB)) + tr_piece;
-    foff[i] = (i < kMB ? 0 : kRows * kM) + tr_row * (i < kMB ? kM : 256) + ((x ^ (4 * (tr_i >> 2))) * 8) + tr_sub;
+    foff[i] = (i < kMB ? 0 : kRows * kM) + tr_row * (i < kMB ? kM : 256) + place_of(x, tr_i >> 2) * 8 + tr_sub;
   }
   bf16x8 pf[2][kMB], qf[2][2];
   auto read_frag = [&](int stage, int kk, int i) {
@@ -125,10 +125,10 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
     if (i < kMB) pf[kk & 1][i] = f;
     else qf[kk & 1][i - kMB] = f;
   };
-  constexpr int kPuts = Stager<kEight, kM>::kN + Stager<true, 256>::kN;
+  constexpr int kPuts = Stager<kEight, kM>::kPuts + Stager<true, 256>::kPuts;
   auto put = [&](int stage, int i) {
-    if (i < qs.kN) qs.put(smem + stage * kStage + kRows * kM, i);
-    else ps.put(smem + stage * kStage, i - qs.kN);
+    if (i < qs.kPuts) qs.put(smem + stage * kStage + kRows * kM, i);
+    else ps.put(smem + stage * kStage, i - qs.kPuts);
   };
   auto request = [&](int step) {
     qs.request((begin + step) * kRows);
@@ -150,8 +150,8 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
 #pragma unroll
   for (int i = 0; i < kFrags; ++i) read_frag(0, 0, i);
   // A step is four quarters of 16 tokens; during a quarter the next one's fragments are read.  In the first half the step
-  // after this one, requested a step ago, goes to the other stage, and the one behind it is requested.  In front of the last
-  // quarter stands the barrier behind which the other stage is whole and this one is read no more.  (Steps past the last
+  // after this one, requested a step ago, goes to the other stage, and the one behind it is requested.  Behind the last quarter's
+  // first product stands the barrier behind which the other stage is whole and this one is read no more.  (Steps past the last
   // read zeros that nobody uses.)
 #pragma unroll 1
   for (int st = 0; st < nsteps; ++st) {
@@ -159,17 +159,18 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
       if (kk == 2) request(st + 2);
-      if (kk == 3) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
 #pragma unroll
       for (int x = 0; x < kMfma; ++x) {
+        acc[x >> 1][x & 1] = mfma32(pf[kk & 1][x >> 1], qf[kk & 1][x & 1], acc[x >> 1][x & 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (kk == 3 && x == 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");   // (under the first products)
 #pragma unroll
         for (int i = x; i < kFrags; i += kMfma) read_frag(kk == 3 ? next : stage, (kk + 1) & 3, i);
         if (kk < 2) {
 #pragma unroll
-          for (int i = kk * kMfma + x; i < kPuts; i += 2 * kMfma) put(next, i);
+          for (int i = 0; i < kPuts; ++i)
+            if (i * (2 * kMfma) / kPuts == kk * kMfma + x) put(next, i);   // (spread evenly over the half's products)
         }
-        __builtin_amdgcn_sched_barrier(0);
-        acc[x >> 1][x & 1] = mfma32(pf[kk & 1][x >> 1], qf[kk & 1][x & 1], acc[x >> 1][x & 1]);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -191,6 +192,123 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
   }
 }
 
+// Few tokens: 64 x 64 tiles by 8 waves that share the tokens, wave w the chunks w, w + 8, ... of 32.  A wave stages its chunk in
+// LDS of its own, so nothing waits for a barrier, requests the next one while it multiplies, and the waves' sums meet in LDS
+// once, w + 4 to w first and then in order.
+constexpr int kChunk = 32;
+template <bool kEight>
+__global__ __launch_bounds__(512, 4) void fp8_wgrad_slice_kernel(Wgrad pr) {
+  constexpr int kArea = 2 * kChunk * 64;   // bf16 elements of a wave: 32 rows of 64 columns of dy, then of x
+  __shared__ __attribute__((aligned(1024))) uint16_t smem[8 * kArea];
+  static_assert(sizeof(smem) == 4 * 64 * 64 * sizeof(float), "the sums of four waves take its place");
+  const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tile = blockIdx.x, tile_m = tile / pr.n_tiles;
+  const int m0 = tile_m * 64, n0 = (tile - tile_m * pr.n_tiles) * 64;
+  uint16_t* const area = smem + wave * kArea;
+  // Piece x (8 columns) of row r at position x ^ 5 (r / 2 % 2): four rows' reads, and the writes of 16 lanes, in different banks.
+  auto place = [](int x, int r) { return r * 64 + ((x ^ (5 * (r >> 1 & 1))) * 8); };
+  constexpr int kPer = kEight ? 4 : 8, kP = kChunk * kPer / 64, kQ = kChunk * 4 / 64;   // lanes per row of dy, loads of dy and x
+  const int64_t ppitch = pr.dy_stride * (kEight ? 1 : 2);
+  const int blocks_p = fp8_blocks(pr.n_out), blocks_q = fp8_blocks(pr.n_in);
+  const int prow = lane / kPer, pcol = lane % kPer * (kEight ? 16 : 8), qrow = lane >> 2, qcol = (lane & 3) * 16;
+  const bool pthere = m0 + pcol < pr.n_out, qthere = n0 + qcol < pr.n_in;
+  const uint32_t poff = pthere ? (uint32_t)prow * (uint32_t)ppitch + pcol * (kEight ? 1 : 2) : 0x80000000u;
+  const uint32_t qoff = qthere ? (uint32_t)qrow * (uint32_t)pr.n_in + qcol : 0x80000000u;
+  const uint32_t psoff = pthere ? (uint32_t)prow * (uint32_t)blocks_p + (m0 + pcol) / kFp8Block : 0x80000000u;
+  const uint32_t qsoff = qthere ? (uint32_t)qrow * (uint32_t)blocks_q + (n0 + qcol) / kFp8Block : 0x80000000u;
+  u32x4 pd[kP], qd[kQ];
+  uint32_t pb[kP] = {}, qb[kQ];
+  auto request = [&](int chunk) {   // (rows at or beyond T: zeros)
+    const int first = min(chunk * kChunk, T), rows = min(T - first, kChunk);
+    const __amdgpu_buffer_rsrc_t p = uniform_rsrc(static_cast<const uint8_t*>(pr.dy) + first * ppitch + (int64_t)m0 * (kEight ? 1 : 2),
+                                                  (uint32_t)rows * (uint32_t)ppitch);
+    const __amdgpu_buffer_rsrc_t q = uniform_rsrc(pr.x + (int64_t)first * pr.n_in + n0, (uint32_t)rows * (uint32_t)pr.n_in);
+    const __amdgpu_buffer_rsrc_t qs = uniform_rsrc(pr.xs + (int64_t)first * blocks_q, (uint32_t)rows * (uint32_t)blocks_q);
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) qd[i] = __builtin_amdgcn_raw_buffer_load_b128(q, qoff, (uint32_t)(16 * i) * (uint32_t)pr.n_in, 0);
+#pragma unroll
+    for (int i = 0; i < kP; ++i)
+      pd[i] = __builtin_amdgcn_raw_buffer_load_b128(p, poff, (uint32_t)(64 / kPer * i) * (uint32_t)ppitch, 0);
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) qb[i] = __builtin_amdgcn_raw_buffer_load_b8(qs, qsoff, (uint32_t)(16 * i) * (uint32_t)blocks_q, 0);
+    if (kEight) {
+      const __amdgpu_buffer_rsrc_t ps = uniform_rsrc(pr.dys + (int64_t)first * blocks_p, (uint32_t)rows * (uint32_t)blocks_p);
+#pragma unroll
+      for (int i = 0; i < kP; ++i) pb[i] = __builtin_amdgcn_raw_buffer_load_b8(ps, psoff, (uint32_t)(16 * i) * (uint32_t)blocks_p, 0);
+    }
+  };
+  auto put8 = [&](uint16_t* to, u32x4 d, uint32_t byte, int row, int col) {
+    *reinterpret_cast<bf16x8*>(to + place(col / 8, row)) = to_bf16x8(d[0], d[1], scale_bits(byte));
+    *reinterpret_cast<bf16x8*>(to + place(col / 8 + 1, row)) = to_bf16x8(d[2], d[3], scale_bits(byte));
+  };
+  // Fragment reads: lane -> row tr_row (+ 8) of 16 and 4 columns of a block of 32
+  const int tr_i = lane & 15, tr_q = lane >> 4;
+  const int tr_row = (tr_i >> 2) + 4 * (tr_q >> 1), tr_piece = 2 * (tr_q & 1) + ((tr_i & 3) >> 1), tr_sub = 4 * (tr_i & 1);
+  f32x16 acc[2][2] = {};
+  const int chunks = (T + kChunk - 1) / kChunk;
+  if (wave < chunks) request(wave);
+  for (int chunk = wave; chunk < chunks; chunk += 8) {
+#pragma unroll
+    for (int i = 0; i < kQ; ++i) put8(area + kChunk * 64, qd[i], qb[i], 16 * i + qrow, qcol);
+#pragma unroll
+    for (int i = 0; i < kP; ++i) {
+      if (kEight) put8(area, pd[i], pb[i], 16 * i + prow, pcol);
+      else *reinterpret_cast<u32x4*>(area + place(pcol / 8, 8 * i + prow)) = pd[i];
+    }
+    if (chunk + 8 < chunks) request(chunk + 8);
+    // (a wave's LDS operations complete in order)
+#pragma unroll
+    for (int kk = 0; kk < kChunk / 16; ++kk) {
+      bf16x8 f[2][2];
+#pragma unroll
+      for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint16_t* from = area + o * (kChunk * 64);
+          const int r = 16 * kk + tr_row, x = 4 * b + tr_piece;
+          f[o][b] = join_tr(lds_read_tr4(from + place(x, r) + tr_sub), lds_read_tr4(from + place(x, r + 8) + tr_sub));
+        }
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) acc[a][b] = mfma32(f[0][a], f[1][b], acc[a][b]);
+    }
+  }
+  float* const sums = reinterpret_cast<float*>(smem);
+  const int l = lane_again(), c = l & 31, g = l >> 5;
+  auto at = [&](int w, int a, int b, int v) { return (w * 64 + a * 32 + 8 * (v >> 2) + 4 * g + (v & 3)) * 64 + b * 32 + c; };
+#pragma unroll
+  for (int round = 0; round < 2; ++round) {   // waves 4 .. 7 hand theirs over, then waves 0 .. 3 the sums of two
+    __syncthreads();
+    if (wave >> 2 == 1 - round) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            float& s = sums[at(wave & 3, a, b, v)];
+            s = round == 0 ? acc[a][b][v] : acc[a][b][v] + s;
+          }
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int p = wave * 64 + l + 512 * i, m = m0 + (p >> 4), n = n0 + (p & 15) * 4;
+    if (m >= pr.n_out || n >= pr.n_in) continue;
+    float4 s = *reinterpret_cast<const float4*>(&sums[p * 4]);
+#pragma unroll
+    for (int w = 1; w < 4; ++w) {
+      const float4 b = *reinterpret_cast<const float4*>(&sums[w * 4096 + p * 4]);
+      s.x += b.x; s.y += b.y; s.z += b.z; s.w += b.w;
+    }
+    *reinterpret_cast<float4*>(pr.out + (int64_t)m * pr.n_in + n) = s;
+  }
+}
+
 // out[i] = sum over splits of partial[s][i], in order, four at a time.
 __global__ __launch_bounds__(256) void fp8_wgrad_add_kernel(const float* __restrict__ partial, int splits, int64_t count4,
                                                             float* __restrict__ out) {
@@ -205,20 +323,26 @@ __global__ __launch_bounds__(256) void fp8_wgrad_add_kernel(const float* __restr
   }
 }
 
-// Splits of the tokens and the tile's height with the least estimated time.
+// Splits of the tokens and the tile's height (0: slices) with the least estimated time.  (Fitted to 16 shapes, which it meets
+// within a fifth.  One piece in slices, tiles of 256 and 128 rows: 64 x 768 x 768 4.9 / 8.5 / 6.3 us, 945 x 768 x 768 8.2 / 26 / 18,
+// 945 x 768 x 2304 13.9 / 27 / 18.7, 945 x 768 x 6144 28 / 29 / 21, 2500 x 768 x 768 14.9 / 57 / 39 (in 5 splits 26 / 20.7), 26963 x
+// 768 x 768 94 / 530 / 359 (24 and 14 splits 47 / 44), 26963 x 768 x 6144 638 / 541 / 380 (3 and 5 splits 226 / 277).)
 struct Choice {
   int splits, height;
 };
 Choice choose(int T_cap, int n_in, int n_out) {
   const int steps = (T_cap + kRows - 1) / kRows;
   const double bytes = 4.0 * n_in * n_out;
-  Choice best{1, 4};
-  double least = 1e300;
+  const double slices = (double)((n_out + 63) / 64) * ((n_in + 63) / 64) / kComputeUnits;
+  Choice best{1, 0};
+  double least = 2.2 + (slices > 1.0 ? slices : 1.0) * (1.7 + 0.85 * ((T_cap + 8 * kChunk - 1) / (8 * kChunk)));
   for (int mb = 4; mb >= 2; mb -= 2) {
     const int64_t tiles = (int64_t)((n_out + 64 * mb - 1) / (64 * mb)) * ((n_in + 255) / 256);
     for (int s = 1; s <= kMaxSplits && s <= (steps > 0 ? steps : 1); ++s) {
-      const double cost = (double)((tiles * s + kComputeUnits - 1) / kComputeUnits) * ((mb == 4 ? 1.5 : 1.1) * ((steps + s - 1) / s) + 6.0) +
-                          (s > 1 ? 4.0 + (2 * s + 1) * bytes / 4.5e6 : 0.0);
+      const double full = tiles * s < kComputeUnits ? (double)(tiles * s) / kComputeUnits : 1.0;
+      const double step = mb == 4 ? 1.25 + 0.35 * full : 0.85 + 0.2 * full;
+      const double cost = 3.0 + (double)((tiles * s + kComputeUnits - 1) / kComputeUnits) * (step * ((steps + s - 1) / s) + 2.5) +
+                          (s > 1 ? 2.5 + (s + 1) * bytes / 7e6 : 0.0);
       if (cost < least) {
         least = cost;
         best = Choice{s, mb};
@@ -246,6 +370,13 @@ mb_status launch_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy
                                   const uint8_t* xs, int T_cap, const int32_t* meta, int n_in, int n_out, float* dw,
                                   void* workspace, hipStream_t stream) {
   const Choice ch = choose(T_cap, n_in, n_out);
+  if (ch.height == 0) {
+    const int n_tiles = (n_in + 63) / 64, tiles = (n_out + 63) / 64 * n_tiles;
+    const Wgrad pr{dy, dys, dy_row_stride, xq, xs, n_out, n_in, n_tiles, tiles, 1, T_cap, meta, dw};
+    if (dys) fp8_wgrad_slice_kernel<true><<<dim3(tiles), dim3(512), 0, stream>>>(pr);
+    else fp8_wgrad_slice_kernel<false><<<dim3(tiles), dim3(512), 0, stream>>>(pr);
+    return check_launch("fp8_wgrad_slice_kernel");
+  }
   const int n_tiles = (n_in + 255) / 256, tiles = (n_out + 64 * ch.height - 1) / (64 * ch.height) * n_tiles;
   const bool whole = ch.splits == 1;
   const Wgrad pr{dy, dys, dy_row_stride, xq, xs, n_out, n_in, n_tiles, tiles, ch.splits, T_cap, meta,
