@@ -66,7 +66,11 @@ struct Product {
   void* out;
   int ldo;                          // elements from row to row
   uint8_t* out_s;                   // kAct: scales [T, gate_row / 128]
+  bool passing;                     // results that no cache will hold: stored non-temporally
 };
+// Results of more than the last level cache, 256 MiB, cannot stay in it for who reads them (8089 x 768 x 30528, 494 MB: 226 us,
+// and 208 stored non-temporally; 26963 x 768 x 768, 41 MB, read again by the next call: 25 and 28.7).
+constexpr int64_t kLastLevelCache = 256 << 20;
 
 // One value GeLU(x W1) (*) x V in 64 bits, by a whole wave: token `row`, column `col`.
 __device__ __forceinline__ double gated_value64(const Product& pr, int row, int col, int lane) {
@@ -466,7 +470,9 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
             const u32x4 w = *reinterpret_cast<const u32x4*>(&slab[r * 64 + ((opiece ^ ((r >> 2) & 3)) * 16)]);
             // (what is out of range: an offset past the descriptor, the store is dropped)
             const uint32_t off = ((uint32_t)t * (uint32_t)pr.ldo + (uint32_t)col) * kEs;
-            __builtin_amdgcn_raw_buffer_store_b128(w, ors, m0 + t < T && col < w_rows ? off : 0xffffffe0u, 0, 0);
+            const uint32_t to = m0 + t < T && col < w_rows ? off : 0xffffffe0u;
+            if (pr.passing) __builtin_amdgcn_raw_buffer_store_b128(w, ors, to, 0, 2);
+            else __builtin_amdgcn_raw_buffer_store_b128(w, ors, to, 0, 0);
           }
         }
       }
@@ -665,7 +671,8 @@ void launch_product(const Product& pr, int cols, hipStream_t stream) {
 mb_status launch_linear_fp8_fwd(const uint8_t* xq, const uint8_t* xs, const uint8_t* wq, const uint8_t* ws, int T_cap,
                                 const int32_t* meta, int n_in, int n_out, mb_dtype y_dt, void* y, int64_t y_row_stride,
                                 hipStream_t stream) {
-  const Product pr{xq, xs, wq, ws, n_in, n_out, 0, 0, T_cap, meta, y, (int)y_row_stride, nullptr};
+  const Product pr{xq, xs, wq, ws, n_in, n_out, 0, 0, T_cap, meta, y, (int)y_row_stride, nullptr,
+                   (int64_t)T_cap * n_out * (int64_t)elem_size(y_dt) > kLastLevelCache};
   if (y_dt == MB_F32) launch_product<kF32>(pr, n_out, stream);
   else launch_product<kBf16>(pr, n_out, stream);
   return check_launch("fp8_gemm_kernel");
@@ -673,7 +680,7 @@ mb_status launch_linear_fp8_fwd(const uint8_t* xq, const uint8_t* xs, const uint
 
 mb_status launch_geglu_fp8_act(const uint8_t* xq, const uint8_t* xs, const uint8_t* w1vq, const uint8_t* w1vs, int T_cap,
                                const int32_t* meta, int hidden, int inter, uint8_t* actq, uint8_t* acts, hipStream_t stream) {
-  const Product pr{xq, xs, w1vq, w1vs, hidden, 2 * inter, 0, inter, T_cap, meta, actq, inter, acts};
+  const Product pr{xq, xs, w1vq, w1vs, hidden, 2 * inter, 0, inter, T_cap, meta, actq, inter, acts, false};
   launch_product<kAct>(pr, 2 * inter, stream);
   return check_launch("fp8_gemm_kernel");
 }

@@ -25,59 +25,69 @@ struct Wgrad {
   float* out;                     // of the first split; split s is n_out n_in floats further on, s times
 };
 
-// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4): the four rows a transposing read touches lie in different
-// banks.  The second 16 pieces of a row lie with even and odd ones exchanged: 16 lanes, each with two pieces of one row from
-// its 16 bytes in 8 bits, write the first of them to different banks so, and then the second.
-__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ (x >> 4 & 1); }
+// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4) ^ 2 (r % 2) ^ x / 16 % 2.  The four rows a transposing read
+// touches lie in different banks, and so do the pieces that 16 lanes, 8 of a row, write at a time of their 32 bytes in 8 bits.
+__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ (2 * (r & 1)) ^ (x >> 4 & 1); }
 
-// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.
+// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.  In 8 bits a thread takes 16 or 32
+// bytes of one row, which have one scale (a load of its own for each 16 bytes took a tenth of the whole time).
 template <bool kEight, int kCols>
 struct Stager {
-  static constexpr int kPerRow = kCols / (kEight ? 16 : 8);   // 16-byte pieces of a row in memory
-  static constexpr int kN = kRows * kPerRow / 512;            // per thread
+  static constexpr int kPieces = kCols / (kEight ? 16 : 8);   // 16-byte pieces of a row in memory
+  static constexpr int kN = kRows * kPieces / 512;            // per thread
+  static constexpr int kLanes = kEight ? 8 : kPieces;         // threads per row
   u32x4 data[kN];
-  uint8_t byte[kN];
-  int row, piece;
-  uint32_t off, soff;       // byte offsets in a step's rows (out of range where the columns end)
+  uint32_t byte;
+  int row, piece;           // of the first; the n-th is the next piece (8 bits), or lies 512 / kLanes rows on
+  uint32_t off, soff;       // byte offsets in a step's rows
+  int there;                // pieces that are columns
   const uint8_t *base, *sbase;
   int64_t pitch;            // bytes from row to row
   int blocks, T;
   __device__ __forceinline__ Stager(const void* p, const uint8_t* s, int64_t stride, int first_col, int cols, int T_, int tid) {
     constexpr int kEs = kEight ? 1 : 2;
-    row = tid / kPerRow;
-    piece = tid % kPerRow;
+    row = tid / kLanes;
+    piece = tid % kLanes * (kEight ? kN : 1);
     pitch = stride * kEs;
     blocks = fp8_blocks(cols);
     T = T_;
-    const int col = piece * (16 / kEs);
-    const bool there = first_col + col < cols;
+    const int col = first_col + piece * (16 / kEs);
+    there = (cols - col) / (16 / kEs);   // (columns are a multiple of 16)
     base = static_cast<const uint8_t*>(p) + (int64_t)first_col * kEs;
-    sbase = kEight ? s : nullptr;
-    off = there ? (uint32_t)row * (uint32_t)pitch + piece * 16 : 0x80000000u;
-    soff = there ? (uint32_t)row * (uint32_t)blocks + (first_col + col) / kFp8Block : 0x80000000u;
+    sbase = s;
+    off = (uint32_t)row * (uint32_t)pitch + piece * 16;
+    soff = there > 0 ? (uint32_t)row * (uint32_t)blocks + col / kFp8Block : 0x80000000u;
   }
-  // requests the rows of 64 tokens from `first` on (rows at or beyond T: zeros)
-  __device__ __forceinline__ void request(int first) {
+  // The rows of 64 tokens from `first` on are what is requested next (rows at or beyond T, and what is no column: zeros).
+  __amdgpu_buffer_rsrc_t rsrc, srsrc;
+  __device__ __forceinline__ void aim(int first) {
     const int rows = max(min(T - first, kRows), 0);
     const int at = rows > 0 ? first : 0;
-    const __amdgpu_buffer_rsrc_t r = uniform_rsrc(base + (int64_t)at * pitch, (uint32_t)rows * (uint32_t)pitch);
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-      data[i] = __builtin_amdgcn_raw_buffer_load_b128(r, off, (uint32_t)(i * (512 / kPerRow)) * (uint32_t)pitch, 0);
-    if (kEight) {
-      const __amdgpu_buffer_rsrc_t q = uniform_rsrc(sbase + (int64_t)at * blocks, (uint32_t)rows * (uint32_t)blocks);
-#pragma unroll
-      for (int i = 0; i < kN; ++i)
-        byte[i] = __builtin_amdgcn_raw_buffer_load_b8(q, soff, (uint32_t)(i * (512 / kPerRow)) * (uint32_t)blocks, 0);
-    }
+    rsrc = uniform_rsrc(base + (int64_t)at * pitch, (uint32_t)rows * (uint32_t)pitch);
+    if (kEight) srsrc = uniform_rsrc(sbase + (int64_t)at * blocks, (uint32_t)rows * (uint32_t)blocks);
+  }
+  __device__ __forceinline__ void request(int i) {
+    data[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, there > (kEight ? i : 0) ? off : 0x80000000u,
+                                                    kEight ? 16 * i : (uint32_t)(i * (512 / kLanes)) * (uint32_t)pitch, 0);
+  }
+  __device__ __forceinline__ void request_scale() {
+    if (kEight) byte = __builtin_amdgcn_raw_buffer_load_b8(srsrc, soff, 0, 0);
+  }
+  // After the i-th put: requests what it was the last to need.
+  __device__ __forceinline__ void request_behind(int i) {
+    if ((i + 1) % kParts == 0) request(i / kParts);
+    if (i + 1 == kPuts) request_scale();
   }
   // brings the i-th 16 bytes of bf16 of what was requested to LDS
   static constexpr int kParts = kEight ? 2 : 1, kPuts = kN * kParts;
   __device__ __forceinline__ void put(uint16_t* to, int i) const {
-    const int n = i / kParts, part = i % kParts, r = row + n * (512 / kPerRow);
-    uint16_t* const at = to + r * kCols + place_of(kParts * piece + part, r) * 8;
-    if (kEight) *reinterpret_cast<bf16x8*>(at) = to_bf16x8(data[n][2 * part], data[n][2 * part + 1], scale_bits(byte[n]));
-    else *reinterpret_cast<u32x4*>(at) = data[n];
+    if (kEight) {
+      *reinterpret_cast<bf16x8*>(to + row * kCols + place_of(2 * piece + i, row) * 8) =
+          to_bf16x8(data[i / 2][i % 2 * 2], data[i / 2][i % 2 * 2 + 1], scale_bits(byte));
+    } else {
+      const int r = row + i * (512 / kLanes);
+      *reinterpret_cast<u32x4*>(to + r * kCols + place_of(piece, r) * 8) = data[i];
+    }
   }
 };
 
@@ -130,9 +140,13 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
     if (i < qs.kPuts) qs.put(smem + stage * kStage + kRows * kM, i);
     else ps.put(smem + stage * kStage, i - qs.kPuts);
   };
-  auto request = [&](int step) {
-    qs.request((begin + step) * kRows);
-    ps.request((begin + step) * kRows);
+  auto aim = [&](int step) {
+    qs.aim((begin + step) * kRows);
+    ps.aim((begin + step) * kRows);
+  };
+  auto request_behind = [&](int i) {
+    if (i < qs.kPuts) qs.request_behind(i);
+    else ps.request_behind(i - qs.kPuts);
   };
   f32x16 acc[kMB][2];   // [m block][n block]
 #pragma unroll
@@ -142,23 +156,28 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
 #pragma unroll
       for (int v = 0; v < 16; ++v) acc[x][y][v] = 0.f;
 
-  request(0);
+  aim(0);
 #pragma unroll
-  for (int i = 0; i < kPuts; ++i) put(0, i);
-  request(1);
+  for (int i = 0; i < kPuts; ++i) request_behind(i);
+  aim(1);
+#pragma unroll
+  for (int i = 0; i < kPuts; ++i) {
+    put(0, i);
+    request_behind(i);
+  }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kFrags; ++i) read_frag(0, 0, i);
-  // A step is four quarters of 16 tokens; during a quarter the next one's fragments are read.  In the first half the step
-  // after this one, requested a step ago, goes to the other stage, and the one behind it is requested.  Behind the last quarter's
-  // first product stands the barrier behind which the other stage is whole and this one is read no more.  (Steps past the last
-  // read zeros that nobody uses.)
+  // A step is four quarters of 16 tokens; during a quarter the next one's fragments are read.  In the first three the step
+  // after this one goes to the other stage, piece by piece, and behind each piece the same one of the step after that is
+  // requested, a whole step before it is needed.  Behind the last quarter's first product stands the barrier behind which the
+  // other stage is whole and this one is read no more.  (Steps past the last read zeros that nobody uses.)
 #pragma unroll 1
   for (int st = 0; st < nsteps; ++st) {
     const int stage = st & 1, next = stage ^ 1;
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      if (kk == 2) request(st + 2);
+      if (kk == 0) aim(st + 2);
 #pragma unroll
       for (int x = 0; x < kMfma; ++x) {
         acc[x >> 1][x & 1] = mfma32(pf[kk & 1][x >> 1], qf[kk & 1][x & 1], acc[x >> 1][x & 1]);
@@ -166,10 +185,12 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
         if (kk == 3 && x == 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");   // (under the first products)
 #pragma unroll
         for (int i = x; i < kFrags; i += kMfma) read_frag(kk == 3 ? next : stage, (kk + 1) & 3, i);
-        if (kk < 2) {
 #pragma unroll
-          for (int i = 0; i < kPuts; ++i)
-            if (i * (2 * kMfma) / kPuts == kk * kMfma + x) put(next, i);   // (spread evenly over the half's products)
+        for (int i = 0; i < kPuts; ++i) {
+          if (i * (3 * kMfma) / kPuts == kk * kMfma + x) {   // (spread evenly over the first three quarters)
+            put(next, i);
+            request_behind(i);
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
