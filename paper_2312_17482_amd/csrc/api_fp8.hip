@@ -38,6 +38,11 @@ mb_status check_stride(int64_t stride, int W, mb_dtype dt, const char* name) {
     if (st_ != MB_OK) return st_;     \
   } while (0)
 
+// (the row kernels count a row's pieces of 16 in 32 bits)
+mb_status check_matrix(int T_cap, int W) {
+  MB_REQUIRE((int64_t)T_cap * W < ((int64_t)1 << 35), MB_ERR_UNSUPPORTED, "matrix of 2^35 elements or more (%d x %d)", T_cap, W);
+  return MB_OK;
+}
 mb_status check_product(int T_cap, int n_in, int n_out) {
   MB_CHECK(check_rows(T_cap));
   MB_CHECK(check_width(n_in, 16, "n_in"));
@@ -56,6 +61,7 @@ mb_status mb_fp8_quant(const void* x, int64_t x_row_stride, int T_cap, const int
   MB_CHECK(check_dtype(dt));
   MB_CHECK(check_rows(T_cap));
   MB_CHECK(check_width(W, 16, "W"));
+  MB_CHECK(check_matrix(T_cap, W));
   MB_CHECK(check_stride(x_row_stride, W, dt, "x_row_stride"));
   if (T_cap == 0) return MB_OK;
   MB_CHECK_PTR(x);
@@ -70,6 +76,7 @@ mb_status mb_fp8_dequant(const uint8_t* q, const uint8_t* s, int T_cap, const in
   MB_CHECK(check_dtype(dt));
   MB_CHECK(check_rows(T_cap));
   MB_CHECK(check_width(W, 16, "W"));
+  MB_CHECK(check_matrix(T_cap, W));
   MB_CHECK(check_stride(x_row_stride, W, dt, "x_row_stride"));
   if (T_cap == 0) return MB_OK;
   MB_CHECK_PTR(q);
@@ -164,6 +171,7 @@ mb_status mb_gelu_gate_fp8_bwd(const void* da, const void* hg, const uint8_t* hg
   clear_error();
   MB_CHECK(check_rows(T_cap));
   MB_CHECK(check_width(inter, 128, "inter"));
+  MB_CHECK(check_matrix(T_cap, inter));
   if (T_cap == 0) return MB_OK;
   MB_CHECK_PTR(da);
   MB_CHECK_PTR(hg);

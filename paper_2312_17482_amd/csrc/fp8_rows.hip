@@ -46,28 +46,40 @@ __device__ __forceinline__ u32x4 pack16(const float (&x)[16], int byte) {
   return r;
 }
 
+// The k-th of the items from `first` (the same in all lanes) on, k < 256, rows of `per` items: its row and place in it.  (Below
+// 512 items a row k crosses several rows: c m / 2^20 with m the next integer over 2^20 / per is c / per exactly for c < 768.  The
+// division of 64-bit numbers that stood here was a fifth of the gate backward's instructions.)
+__device__ __forceinline__ void locate(uint32_t first, uint32_t per, uint32_t k, int64_t& row, int& at) {
+  const uint32_t row0 = __builtin_amdgcn_readfirstlane(first / per);
+  const uint32_t c = first - row0 * per + k;
+  const uint32_t m = __builtin_amdgcn_readfirstlane((1u << 20) / per + 1);
+  const uint32_t rows = per > 512 ? (c >= per ? 1u : 0u) : (c * m) >> 20;
+  row = (int64_t)row0 + rows;
+  at = (int)(c - rows * per);
+}
+
 // Rows -> 8 bits: eight lanes per block of 128, 16 values each.
 template <typename T>
 __global__ __launch_bounds__(256) void fp8_quant_kernel(const T* __restrict__ x, int64_t stride, int T_cap,
                                                         const int32_t* __restrict__ meta, int W, int blocks,
                                                         uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
   const int rows = meta ? min(meta[0], T_cap) : T_cap;
-  const int64_t total = (int64_t)rows * blocks;
   const int piece = threadIdx.x & 7;
-  for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3; at < total; at += (int64_t)gridDim.x * 32) {
-    const int64_t row = at / blocks;
-    const int col = (int)(at - row * blocks) * kFp8Block + piece * 16;
-    float v[16];
-    if (col < W) {
-      load16(x + row * stride + col, v);
-    } else {
+  int64_t row;
+  int block;
+  locate(blockIdx.x * 32, blocks, threadIdx.x >> 3, row, block);
+  if (row >= rows) return;
+  const int col = block * kFp8Block + piece * 16;
+  float v[16];
+  if (col < W) {
+    load16(x + row * stride + col, v);
+  } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = 0.f;
-    }
-    const int byte = scale_byte(max_of_8_lanes(largest_of_16(v)));
-    if (col < W) *reinterpret_cast<u32x4*>(q + row * W + col) = pack16(v, byte);
-    if (piece == 0) s[at] = (uint8_t)byte;
+    for (int i = 0; i < 16; ++i) v[i] = 0.f;
   }
+  const int byte = scale_byte(max_of_8_lanes(largest_of_16(v)));
+  if (col < W) *reinterpret_cast<u32x4*>(q + row * W + col) = pack16(v, byte);
+  if (piece == 0) s[row * blocks + block] = (uint8_t)byte;
 }
 
 // 8-bit rows -> rows: 16 values per lane.
@@ -76,23 +88,22 @@ __global__ __launch_bounds__(256) void fp8_dequant_kernel(const uint8_t* __restr
                                                           int T_cap, const int32_t* __restrict__ meta, int W, int blocks,
                                                           T* __restrict__ x, int64_t stride) {
   const int rows = meta ? min(meta[0], T_cap) : T_cap;
-  const int pieces = W >> 4;
-  const int64_t total = (int64_t)rows * pieces;
-  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
-    const int64_t row = at / pieces;
-    const int col = (int)(at - row * pieces) * 16;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(q + row * W + col);
-    const float scale = scale_bits(s[row * blocks + (col >> 7)]);
-    float v[16];
+  int64_t row;
+  int piece;
+  locate(blockIdx.x * 256, W >> 4, threadIdx.x, row, piece);
+  if (row >= rows) return;
+  const int col = piece * 16;
+  const u32x4 w = *reinterpret_cast<const u32x4*>(q + row * W + col);
+  const float scale = scale_bits(s[row * blocks + (col >> 7)]);
+  float v[16];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float f[4];
-      unpack_e4m3(w[i], scale, f);
+  for (int i = 0; i < 4; ++i) {
+    float f[4];
+    unpack_e4m3(w[i], scale, f);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) v[4 * i + j] = f[j];
-    }
-    store16(x + row * stride + col, v);
+    for (int j = 0; j < 4; ++j) v[4 * i + j] = f[j];
   }
+  store16(x + row * stride + col, v);
 }
 
 // One 128 x 128 block of a weight per workgroup: thread t holds rows 4 (t / 8) .. + 3, columns 16 (t % 8) .. + 15.  The
@@ -164,83 +175,80 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
                                                            uint8_t* __restrict__ q, uint8_t* __restrict__ s) {
   const int rows = meta ? min(meta[0], T_cap) : T_cap;
   const int blocks = inter / kFp8Block;
-  const int64_t total = (int64_t)rows * blocks;
   const int piece = threadIdx.x & 7;
-  for (int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) >> 3; at < total; at += (int64_t)gridDim.x * 32) {
-    const int64_t row = at / blocks;
-    const int block = (int)(at - row * blocks), col = block * kFp8Block + piece * 16;
-    float a[16], h[16], g[16];
-    load16(da + row * inter + col, a);
-    const int64_t place = row * (2 * inter) + col;
-    if (kEight) {
-      const uint8_t* p = static_cast<const uint8_t*>(hg) + place;
-      const u32x4 hw = *reinterpret_cast<const u32x4*>(p), gw = *reinterpret_cast<const u32x4*>(p + inter);
-      const uint8_t* sc = hgs + row * (2 * blocks) + block;
-      const float hs = scale_bits(sc[0]), gs = scale_bits(sc[blocks]);
+  int64_t row;
+  int block;
+  locate(blockIdx.x * 32, blocks, threadIdx.x >> 3, row, block);
+  if (row >= rows) return;
+  const int col = block * kFp8Block + piece * 16;
+  float a[16], h[16], g[16];
+  load16(da + row * inter + col, a);
+  const int64_t place = row * (2 * inter) + col;
+  if (kEight) {
+    const uint8_t* p = static_cast<const uint8_t*>(hg) + place;
+    const u32x4 hw = *reinterpret_cast<const u32x4*>(p), gw = *reinterpret_cast<const u32x4*>(p + inter);
+    const uint8_t* sc = hgs + row * (2 * blocks) + block;
+    const float hs = scale_bits(sc[0]), gs = scale_bits(sc[blocks]);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float f[4], e[4];
-        unpack_e4m3(hw[i], hs, f);
-        unpack_e4m3(gw[i], gs, e);
+    for (int i = 0; i < 4; ++i) {
+      float f[4], e[4];
+      unpack_e4m3(hw[i], hs, f);
+      unpack_e4m3(gw[i], gs, e);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          h[4 * i + j] = f[j];
-          g[4 * i + j] = e[j];
-        }
+      for (int j = 0; j < 4; ++j) {
+        h[4 * i + j] = f[j];
+        g[4 * i + j] = e[j];
       }
-    } else {
-      const uint16_t* p = static_cast<const uint16_t*>(hg) + place;
-      load16(p, h);
-      load16(p + inter, g);
     }
+  } else {
+    const uint16_t* p = static_cast<const uint16_t*>(hg) + place;
+    load16(p, h);
+    load16(p + inter, g);
+  }
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      float val, grad;
-      gelu_tail_and_grad(h[i], val, grad);
-      h[i] = a[i] * g[i] * grad;
-      g[i] = a[i] * val;
-    }
-    float htop = max_of_8_lanes(largest_of_16(h)), gtop = max_of_8_lanes(largest_of_16(g));
-    if (__builtin_expect(__ballot(near_border(htop, kReach) || near_border(gtop, kReach)) != 0, 0)) {
-      // a block in some thousand: its largest values once more, in 64 bits
-      float h64 = 0.f, g64 = 0.f;
+  for (int i = 0; i < 16; ++i) {
+    float val, grad;
+    gelu_tail_and_grad(h[i], val, grad);
+    h[i] = a[i] * g[i] * grad;
+    g[i] = a[i] * val;
+  }
+  float htop = max_of_8_lanes(largest_of_16(h)), gtop = max_of_8_lanes(largest_of_16(g));
+  if (__builtin_expect(__ballot(near_border(htop, kReach) || near_border(gtop, kReach)) != 0, 0)) {
+    // a block in some thousand: its largest values once more, in 64 bits
+    float h64 = 0.f, g64 = 0.f;
 #pragma unroll 1
-      for (int i = 0; i < 16; ++i) {
-        const double x = bf16_value(da[row * inter + col + i]);
-        double hv, gv, slope;
-        if (kEight) {
-          const uint8_t* p = static_cast<const uint8_t*>(hg) + place + i;
-          const uint8_t* sc = hgs + row * (2 * blocks) + block;
-          hv = (double)__builtin_amdgcn_cvt_f32_fp8(p[0], 0) * scale_value(sc[0]);
-          gv = (double)__builtin_amdgcn_cvt_f32_fp8(p[inter], 0) * scale_value(sc[blocks]);
-        } else {
-          const uint16_t* p = static_cast<const uint16_t*>(hg) + place + i;
-          hv = bf16_value(p[0]);
-          gv = bf16_value(p[inter]);
-        }
-        const double value = gelu64(hv, &slope);
-        h64 = fmaxf(h64, finite_abs(round_beside_border(x * gv * slope)));
-        g64 = fmaxf(g64, finite_abs(round_beside_border(x * value)));
+    for (int i = 0; i < 16; ++i) {
+      const double x = bf16_value(da[row * inter + col + i]);
+      double hv, gv, slope;
+      if (kEight) {
+        const uint8_t* p = static_cast<const uint8_t*>(hg) + place + i;
+        const uint8_t* sc = hgs + row * (2 * blocks) + block;
+        hv = (double)__builtin_amdgcn_cvt_f32_fp8(p[0], 0) * scale_value(sc[0]);
+        gv = (double)__builtin_amdgcn_cvt_f32_fp8(p[inter], 0) * scale_value(sc[blocks]);
+      } else {
+        const uint16_t* p = static_cast<const uint16_t*>(hg) + place + i;
+        hv = bf16_value(p[0]);
+        gv = bf16_value(p[inter]);
       }
-      h64 = max_of_8_lanes(h64);
-      g64 = max_of_8_lanes(g64);
-      if (near_border(htop, kReach)) htop = h64;
-      if (near_border(gtop, kReach)) gtop = g64;
+      const double value = gelu64(hv, &slope);
+      h64 = fmaxf(h64, finite_abs(round_beside_border(x * gv * slope)));
+      g64 = fmaxf(g64, finite_abs(round_beside_border(x * value)));
     }
-    const int hb = scale_byte(htop), gb = scale_byte(gtop);
-    *reinterpret_cast<u32x4*>(q + place) = pack16(h, hb);
-    *reinterpret_cast<u32x4*>(q + place + inter) = pack16(g, gb);
-    if (piece == 0) {
-      s[row * (2 * blocks) + block] = (uint8_t)hb;
-      s[row * (2 * blocks) + blocks + block] = (uint8_t)gb;
-    }
+    h64 = max_of_8_lanes(h64);
+    g64 = max_of_8_lanes(g64);
+    if (near_border(htop, kReach)) htop = h64;
+    if (near_border(gtop, kReach)) gtop = g64;
+  }
+  const int hb = scale_byte(htop), gb = scale_byte(gtop);
+  *reinterpret_cast<u32x4*>(q + place) = pack16(h, hb);
+  *reinterpret_cast<u32x4*>(q + place + inter) = pack16(g, gb);
+  if (piece == 0) {
+    s[row * (2 * blocks) + block] = (uint8_t)hb;
+    s[row * (2 * blocks) + blocks + block] = (uint8_t)gb;
   }
 }
 
-unsigned grid_for(int64_t threads) {
-  const int64_t blocks = (threads + 255) / 256;
-  return (unsigned)(blocks < 65536 ? blocks : 65536);
-}
+unsigned grid_for(int64_t threads) { return (unsigned)((threads + 255) / 256); }
 
 }  // namespace
 
