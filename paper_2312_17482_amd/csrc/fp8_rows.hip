@@ -214,10 +214,19 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
   }
   float htop = max_of_8_lanes(largest_of_16(h)), gtop = max_of_8_lanes(largest_of_16(g));
   if (__builtin_expect(__ballot(near_border(htop, kReach) || near_border(gtop, kReach)) != 0, 0)) {
-    // a block in some thousand: its largest values once more, in 64 bits
+    // a block in some thousand: the values that decide once more, in 64 bits, each lane one of its own after the other
+    const float hfrom = near_border(htop, kReach) ? border_from(htop, kReach) : __builtin_inff();
+    const float gfrom = near_border(gtop, kReach) ? border_from(gtop, kReach) : __builtin_inff();
+    uint32_t left = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      left |= finite_abs(h[i]) >= hfrom ? 1u << i : 0u;
+      left |= finite_abs(g[i]) >= gfrom ? 0x10000u << i : 0u;
+    }
     float h64 = 0.f, g64 = 0.f;
 #pragma unroll 1
-    for (int i = 0; i < 16; ++i) {
+    for (; __ballot(left != 0); left &= left - 1) {
+      const int bit = left ? __builtin_ctz(left) : 0, i = bit & 15;
       const double x = bf16_value(da[row * inter + col + i]);
       double hv, gv, slope;
       if (kEight) {
@@ -231,8 +240,9 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
         gv = bf16_value(p[inter]);
       }
       const double value = gelu64(hv, &slope);
-      h64 = fmaxf(h64, finite_abs(round_beside_border(x * gv * slope)));
-      g64 = fmaxf(g64, finite_abs(round_beside_border(x * value)));
+      const float top = finite_abs(round_beside_border(x * (bit < 16 ? gv * slope : value)));
+      if (left && bit < 16) h64 = fmaxf(h64, top);
+      if (left && bit >= 16) g64 = fmaxf(g64, top);
     }
     h64 = max_of_8_lanes(h64);
     g64 = max_of_8_lanes(g64);

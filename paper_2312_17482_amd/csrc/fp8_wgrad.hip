@@ -13,7 +13,7 @@ namespace mb {
 namespace {
 
 constexpr int kRows = 64;         // tokens per step
-constexpr int kMaxSplits = 32;
+constexpr int kMaxSplits = 128;
 
 struct Wgrad {
   const void* dy;                 // bf16 [T, n_out] of row stride dy_stride, or e4m3 with scales dys
@@ -330,18 +330,37 @@ __global__ __launch_bounds__(512, 4) void fp8_wgrad_slice_kernel(Wgrad pr) {
   }
 }
 
-// out[i] = sum over splits of partial[s][i], in order, four at a time.
+// out[i] = sum over splits of partial[s][i], four at a time: kGroups groups of threads take an equal share of the splits each,
+// in order, and then their sums are added in order.  (With many splits there are few results: one thread for all of a result's
+// would add up one round trip after the other.)
+template <int kGroups>
 __global__ __launch_bounds__(256) void fp8_wgrad_add_kernel(const float* __restrict__ partial, int splits, int64_t count4,
                                                             float* __restrict__ out) {
+  constexpr int kItems = 256 / kGroups;
+  __shared__ float4 sums[kGroups > 1 ? 256 : 1];
   const float4* src = reinterpret_cast<const float4*>(partial);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count4; i += (int64_t)gridDim.x * 256) {
-    float4 a = src[i];
-    for (int s = 1; s < splits; ++s) {
+  const int item = threadIdx.x % kItems, group = threadIdx.x / kItems;
+  const int64_t i = (int64_t)blockIdx.x * kItems + item;
+  const int share = (splits + kGroups - 1) / kGroups, from = group * share, to = min(from + share, splits);
+  float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (i < count4) {
+#pragma unroll 4
+    for (int s = from; s < to; ++s) {
       const float4 b = src[(int64_t)s * count4 + i];
       a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
     }
-    reinterpret_cast<float4*>(out)[i] = a;
   }
+  if (kGroups > 1) {
+    sums[threadIdx.x] = a;
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int g = 1; g < kGroups; ++g) {
+      const float4 b = sums[g * kItems + item];
+      a.x += b.x; a.y += b.y; a.z += b.z; a.w += b.w;
+    }
+  }
+  if (i < count4) reinterpret_cast<float4*>(out)[i] = a;
 }
 
 // Splits of the tokens and the tile's height (0: slices) with the least estimated time.  (Fitted to 16 shapes, which it meets
@@ -406,8 +425,11 @@ mb_status launch_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy
   else launch_wgrad<false>(pr, ch.height, stream);
   if (!whole) {
     const int64_t count4 = (int64_t)n_in * n_out / 4;
-    fp8_wgrad_add_kernel<<<dim3((unsigned)(count4 < 2048 * 256 ? (count4 + 255) / 256 : 2048)), dim3(256), 0, stream>>>(
-        static_cast<const float*>(workspace), ch.splits, count4, dw);
+    const float* partial = static_cast<const float*>(workspace);
+    if (ch.splits >= 8)
+      fp8_wgrad_add_kernel<8><<<dim3((unsigned)((count4 + 31) / 32)), dim3(256), 0, stream>>>(partial, ch.splits, count4, dw);
+    else
+      fp8_wgrad_add_kernel<1><<<dim3((unsigned)((count4 + 255) / 256)), dim3(256), 0, stream>>>(partial, ch.splits, count4, dw);
   }
   return check_launch("fp8_wgrad_kernel");
 }
