@@ -13,6 +13,8 @@
 // A step's rows are 128 bytes, as in the bf16 products, and travel the same way: straight from memory into LDS, one workgroup of
 // 8 waves per compute unit for all its tiles, the loads of a tile's first steps under the last products of the tile before it.
 // A lane owns runs of 4 consecutive output columns of one token (weight rows along accumulator rows, tokens along lanes).
+#include <cmath>
+
 #include "fp8_util.h"
 
 namespace mb {
@@ -488,11 +490,31 @@ __global__ __launch_bounds__(128 * kWN, kWN / 2) void fp8_gemm_kernel(Product pr
   fp8_tiles<kMode, kMB, kWN, kNB, kStages, kDepth>(pr, T, smem, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
-// Products of few rows, whose time is that of the way to memory and back: 16 kA tokens x 16 kB columns by 8 waves that share the
+// Products of a few rows, whose time is that of the way to memory and back: 16 kA tokens x 16 kB columns by 8 waves that share the
 // contraction, wave w its blocks w, w + 8, ... of 128 k.  No stages and no barrier in it: a wave requests a block's rows straight
 // into the registers the matrix instruction reads (v_mfma_scale_f32_16x16x128_f8f6f4, one a block; exact: four of
 // v_mfma_f32_16x16x32_bf16), the next block's while it multiplies, and the waves' sums meet in LDS once, added in order.
 constexpr int kSliceWaves = 8;
+
+// Where piece p (4 columns) of token t's sums lies: the pieces of neighbouring tokens in different banks.
+template <int kPieces>
+__device__ __forceinline__ int sum_place(int t, int p) { return (t * kPieces + (p ^ (t & (kPieces - 1)))) * 4; }
+// The waves' sums of a tile of kTM tokens x kTN columns, added in order, on their way out.
+template <int kMode, int kTM, int kTN, int kThreads>
+__device__ __forceinline__ void store_sums(const Product& pr, const float* sums, int waves, int m0, int n0, int T) {
+  constexpr int kEs = kMode == kF32 ? 4 : 2, kPieces = kTN / 4;
+  uint8_t* const out = static_cast<uint8_t*>(pr.out);
+  for (int at = threadIdx.x; at < kTM * kPieces; at += kThreads) {
+    const int t = at / kPieces, p = at % kPieces, col = n0 + 4 * p;
+    if (m0 + t >= T || col >= pr.w_rows) continue;
+    f32x4 v = *reinterpret_cast<const f32x4*>(&sums[sum_place<kPieces>(t, p)]);
+    for (int i = 1; i < waves; ++i) v += *reinterpret_cast<const f32x4*>(&sums[i * kTM * kTN + sum_place<kPieces>(t, p)]);
+    uint8_t* const to = out + ((int64_t)(m0 + t) * pr.ldo + col) * kEs;
+    if constexpr (kMode == kF32) *reinterpret_cast<f32x4*>(to) = v;
+    else *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  }
+}
+
 template <int kMode, int kA, int kB>
 __global__ __launch_bounds__(64 * kSliceWaves) void fp8_slice_kernel(Product pr) {
   constexpr bool kExact = is_exact(kMode);
@@ -567,32 +589,136 @@ __global__ __launch_bounds__(64 * kSliceWaves) void fp8_slice_kernel(Product pr)
     if (kb + 2 * kSliceWaves < blocks) request(now, kb + 2 * kSliceWaves);
     multiply(ahead);
   }
-  // Lane (c, g) holds columns 16 j + 4 g .. + 3 of token 16 i + c: piece 4 j + g of the token's row (at place ^ token, so that
-  // the 16 tokens' pieces lie in different banks).
-  auto place = [](int t, int p) { return (t * kPieces + (p ^ (t & (kPieces - 1)))) * 4; };
+  // Lane (c, g) holds columns 16 j + 4 g .. + 3 of token 16 i + c.
   if (wave < blocks) {
 #pragma unroll
     for (int i = 0; i < kA; ++i)
 #pragma unroll
       for (int j = 0; j < kB; ++j)
-        *reinterpret_cast<f32x4*>(&sums[wave * kTM * kTN + place(16 * i + c, 4 * j + g)]) = acc[i][j];
+        *reinterpret_cast<f32x4*>(&sums[wave * kTM * kTN + sum_place<kPieces>(16 * i + c, 4 * j + g)]) = acc[i][j];
   }
   __syncthreads();
-  const int waves = min(blocks, kSliceWaves);
-  constexpr int kEs = kMode == kF32 ? 4 : 2;
-  uint8_t* const out = static_cast<uint8_t*>(pr.out);
-  for (int at = tid; at < kTM * kPieces; at += 64 * kSliceWaves) {
-    const int t = at / kPieces, p = at % kPieces, col = n0 + 4 * p;
-    if (m0 + t >= T || col >= w_rows) continue;
-    f32x4 v = *reinterpret_cast<const f32x4*>(&sums[place(t, p)]);
-    for (int i = 1; i < waves; ++i) v += *reinterpret_cast<const f32x4*>(&sums[i * kTM * kTN + place(t, p)]);
-    uint8_t* const to = out + ((int64_t)(m0 + t) * pr.ldo + col) * kEs;
-    if constexpr (kMode == kF32) {
-      *reinterpret_cast<f32x4*>(to) = v;
-    } else {
-      *reinterpret_cast<u32x2*>(to) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  store_sums<kMode, kTM, kTN, 64 * kSliceWaves>(pr, sums, min(blocks, kSliceWaves), m0, n0, T);
+}
+
+// The same with the operands' way through LDS, for products of some hundred rows, where the direct way's 64 bytes of a row at a
+// time are the bound (14 bytes a cycle and compute unit): 32 kA tokens x 32 kB columns by kW waves, each with two stages of its
+// own that it fills itself by whole 128-byte lines.  A wave waits for its own loads only; no barrier until the sums meet.
+template <int kMode, int kA, int kB, int kW>
+__global__ __launch_bounds__(64 * kW) void fp8_ring_kernel(Product pr) {
+  constexpr bool kExact = is_exact(kMode);
+  constexpr int kTM = 32 * kA, kTN = 32 * kB, kPieces = kTN / 4, kRows = kTM + kTN;
+  constexpr int kStage = kRows * kStep + 512;      // rows, 64 words of token scales, 64 of the weight's (all alike)
+  constexpr int kLoads = kRows / 8 + 2;
+  static_assert(kTM <= 64 && kTN <= 128 && 2 * kStage >= kTM * kTN * 4, "one load brings the scales; the sums take the stages' place");
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kW * 2 * kStage];
+  const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
+  const int m0 = blockIdx.y * kTM, n0 = blockIdx.x * kTN;
+  if (m0 >= T) return;
+  const int K = pr.K, blocks = fp8_blocks(K), w_rows = pr.w_rows;
+  const int lane = threadIdx.x & 63, c = lane & 31, g = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int xrows = min(T - m0, kTM);
+  u32x4 xr = raw_rsrc(pr.x + (int64_t)m0 * K, (uint32_t)xrows * (uint32_t)K);
+  u32x4 wr = raw_rsrc(pr.w + (int64_t)n0 * K, (uint32_t)min(w_rows - n0, kTN) * (uint32_t)K);
+  u32x4 xsr = raw_rsrc(pr.xs + (int64_t)m0 * blocks, (uint32_t)xrows * (uint32_t)blocks);
+  u32x4 wsr = raw_rsrc(pr.ws + (int64_t)(n0 / kFp8Block) * blocks, (uint32_t)blocks);
+  // As in the tiles: 8 rows of 8 pieces a load, piece x of row r at position x ^ (r / 2) % 8.
+  const int piece[2] = {(lane & 7) ^ (lane >> 4), (lane & 7) ^ (4 + (lane >> 4))};   // even and odd loads
+  const uint32_t row_off = (uint32_t)(lane >> 3) * (uint32_t)K;
+  const uint32_t lds0 = (uint32_t)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) uint8_t*)smem) + wave * (2 * kStage);
+  auto fetch = [&](int kb, int stage) {
+    uint32_t at = kb * kStep, to = lds0 + stage * kStage;
+    asm("" : "+s"(at), "+s"(to));   // (scalars, and not parts of the lanes' own sums)
+    const uint32_t off[2] = {kb * kStep + piece[0] * 16 < K ? row_off + piece[0] * 16 : 0x80000000u,
+                             kb * kStep + piece[1] * 16 < K ? row_off + piece[1] * 16 : 0x80000000u};
+#pragma unroll
+    for (int i = 0; i < kRows / 8; ++i)
+      load_to_lds(to + 8 * i * kStep, off[i & 1], i < kTM / 8 ? xr : wr,
+                  (uint32_t)(8 * (i < kTM / 8 ? i : i - kTM / 8)) * (uint32_t)K + at);
+    load_byte_to_lds(to + kRows * kStep, (uint32_t)lane * (uint32_t)blocks, xsr, kb);
+    load_byte_to_lds(to + kRows * kStep + 256, 0u, wsr, kb);
+  };
+  uint32_t frag[4];
+#pragma unroll
+  for (int p = 0; p < 4; ++p) frag[p] = c * kStep + (((2 * p + g) ^ ((c >> 1) & 7)) * 16);
+  f32x16 acc[kA][kB] = {};
+  if (wave < blocks) {
+    fetch(wave, 0);
+    if (wave + kW >= blocks) xr[2] = wr[2] = xsr[2] = wsr[2] = 0u;   // (past the end the loads bring nothing; their number stays)
+    fetch(wave + kW, 1);
+    int stage = 0;
+#pragma unroll 1
+    for (int kb = wave; kb < blocks; kb += kW) {
+      asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
+      const uint8_t* const from = smem + wave * (2 * kStage) + stage * kStage;
+      i32x8 f[2][kA + kB];
+      uint32_t sx[kA];
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < kA + kB; ++i) {
+          const u32x4 a = *reinterpret_cast<const u32x4*>(from + i * 32 * kStep + frag[2 * h]);
+          const u32x4 b = *reinterpret_cast<const u32x4*>(from + i * 32 * kStep + frag[2 * h + 1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            f[h][i][e] = (int)a[e];
+            f[h][i][4 + e] = (int)b[e];
+          }
+        }
+      const uint32_t* const sc = reinterpret_cast<const uint32_t*>(from + kRows * kStep);
+#pragma unroll
+      for (int i = 0; i < kA; ++i) sx[i] = sc[32 * i + c];
+      const uint32_t sw = sc[64];
+      asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // (read: the stage may be filled again)
+      if (kb + 2 * kW >= blocks) xr[2] = wr[2] = xsr[2] = wsr[2] = 0u;
+      fetch(kb + 2 * kW, stage);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if constexpr (kExact) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) {
+            bf16x8 xb[kA];
+#pragma unroll
+            for (int i = 0; i < kA; ++i) xb[i] = to_bf16x8(f[h][i][2 * p], f[h][i][2 * p + 1], scale_bits(sx[i]));
+#pragma unroll
+            for (int j = 0; j < kB; ++j) {
+              const bf16x8 wb = to_bf16x8(f[h][kA + j][2 * p], f[h][kA + j][2 * p + 1], scale_bits(sw));
+#pragma unroll
+              for (int i = 0; i < kA; ++i) acc[i][j] = mfma32(wb, xb[i], acc[i][j]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kB; ++j)
+#pragma unroll
+            for (int i = 0; i < kA; ++i) acc[i][j] = mfma_scaled(f[h][kA + j], f[h][i], acc[i][j], sw, sx[i]);
+        }
+      }
+      stage ^= 1;
     }
   }
+  asm volatile("s_waitcnt vmcnt(0)" : : : "memory");   // no load is on its way any more to where the sums go
+  __syncthreads();
+  float* const sums = reinterpret_cast<float*>(smem);
+  if (wave < blocks) {   // lane (c, g): columns 32 j + 8 v + 4 g .. + 3 of token 32 i + c
+#pragma unroll
+    for (int i = 0; i < kA; ++i)
+#pragma unroll
+      for (int j = 0; j < kB; ++j)
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          *reinterpret_cast<f32x4*>(&sums[wave * kTM * kTN + sum_place<kPieces>(32 * i + c, 8 * j + 2 * v + g)]) =
+              f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
+  }
+  __syncthreads();
+  store_sums<kMode, kTM, kTN, 64 * kW>(pr, sums, min(blocks, kW), m0, n0, T);
+}
+
+template <int kMode, int kA, int kB, int kW>
+void launch_rings(const Product& pr, hipStream_t stream) {
+  const dim3 grid((pr.w_rows + 32 * kB - 1) / (32 * kB), (pr.T_cap + 32 * kA - 1) / (32 * kA));
+  fp8_ring_kernel<kMode, kA, kB, kW><<<grid, dim3(64 * kW), 0, stream>>>(pr);
 }
 
 template <int kMode, int kA, int kB>
@@ -621,12 +747,19 @@ double tile_cost(int T, int cols, int K, int mb) {
   const double product = step[mb] * (is_exact(kMode) ? 1.6 : 1.0) * fp8_blocks(K) + ends[mb] + (kMode == kAct ? gate[mb] : 0.0);
   return 3.5 + (double)((tiles + kComputeUnits - 1) / kComputeUnits) * product;
 }
-// The same in slices of 16 a tokens x 16 b columns, which come at 30 KB a microsecond and compute unit.  (1 x 1024 x 4096 in
-// slices of 1 x 1: 3.4 us, in 64 x 256 tiles 7.6; 64 x 4096 x 1024: 1 x 1 7.3, 2 x 2 11.5, tiles 19.5; 300 x 768 x 768: 2 x 2 4.2, 1 x 1
-// 5.6, tiles 6.9; 945 x 768 x 768: 4 x 4 6.2, 2 x 2 7.6, tiles 7.0; 945 x 768 x 2304: 4 x 4 15.0, tiles 7.7.)
-double slice_cost(int T, int cols, int K, int a, int b) {
-  const int64_t groups = ((int64_t)T + 16 * a - 1) / (16 * a) * ((cols + 16 * b - 1) / (16 * b));
-  return 2.2 + (double)((groups + kComputeUnits - 1) / kComputeUnits) * (16.0 * (a + b) * K / 30e3);
+// The same in slices of 16 x 16, which come at 30 KB a microsecond and compute unit, and in rings of 32 a x 32 b: rounds, of a start
+// and an end and a block of each wave each (two workgroups of 32 x 32 fit a compute unit).  (Slices, rings of 1 x 1, 1 x 2, 2 x 2,
+// tiles of 64 x 256: 1 x 1024 x 4096 3.5 / 3.8 / 4.4 / 5.4 / 7.7 us, 64 x 4096 x 1024 7.3 / 6.1 / 7.7 / 10.1 / 19.5, 300 x 768 x 768 5.6 / 3.8 / 4.6 /
+// 5.9 / 7.0, 500 x 3072 x 768 20 / 8.3 / 7.4 / 9.1 / 16.8, 685 x 2304 x 768 22 / 9.2 / 10.4 / 8.3 / 12.8, 945 x 768 x 2304 28 / 16 / 17 / 15 / 7.8.)
+double slice_cost(int T, int cols, int K) {
+  const int64_t groups = ((int64_t)T + 15) / 16 * ((cols + 15) / 16);
+  return 2.2 + (double)((groups + kComputeUnits - 1) / kComputeUnits) * (32.0 * K / 30e3);
+}
+double ring_cost(int T, int cols, int K, int a, int b) {
+  const double groups = (double)(((int64_t)T + 32 * a - 1) / (32 * a) * ((cols + 32 * b - 1) / (32 * b))) / kComputeUnits;
+  const int turns = (fp8_blocks(K) + 3) / 4;
+  if (a == 1 && b == 1) return 2.0 + (groups > 1.0 ? groups : 1.0) * (0.9 + 0.4 * turns);
+  return (a == 1 ? 2.2 : 2.5) + std::ceil(groups) * (a == 1 ? 1.4 + 0.6 * turns : 2.4 + 0.8 * turns);
 }
 
 // The way with the least estimate, by the sizes alone.
@@ -644,16 +777,16 @@ void launch_product(const Product& pr, int cols, hipStream_t stream) {
   for (int mb = 1; mb <= (is_exact(kMode) ? 3 : 4); ++mb) offer(mb, tile_cost<kMode>(T, cols, K, mb));
   if constexpr (kMode != kAct) {
     if (T <= 4096) {   // (a grid has 65535 rows of workgroups at most; never the least beyond)
-      offer(11, slice_cost(T, cols, K, 1, 1));
-      offer(22, slice_cost(T, cols, K, 2, 2));
-      offer(24, slice_cost(T, cols, K, 2, 4));
-      offer(44, slice_cost(T, cols, K, 4, 4));
+      offer(11, slice_cost(T, cols, K));
+      offer(132, ring_cost(T, cols, K, 1, 1));
+      offer(164, ring_cost(T, cols, K, 1, 2));
+      offer(264, ring_cost(T, cols, K, 2, 2));
     }
     switch (best) {
       case 11: return launch_slices<kMode, 1, 1>(pr, stream);
-      case 22: return launch_slices<kMode, 2, 2>(pr, stream);
-      case 24: return launch_slices<kMode, 2, 4>(pr, stream);
-      case 44: return launch_slices<kMode, 4, 4>(pr, stream);
+      case 132: return launch_rings<kMode, 1, 1, 4>(pr, stream);
+      case 164: return launch_rings<kMode, 1, 2, 4>(pr, stream);
+      case 264: return launch_rings<kMode, 2, 2, 4>(pr, stream);
       default: break;
     }
   }
