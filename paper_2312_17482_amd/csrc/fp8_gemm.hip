@@ -13,8 +13,6 @@
 // A step's rows are 128 bytes, as in the bf16 products, and travel the same way: straight from memory into LDS, one workgroup of
 // 8 waves per compute unit for all its tiles, the loads of a tile's first steps under the last products of the tile before it.
 // A lane owns runs of 4 consecutive output columns of one token (weight rows along accumulator rows, tokens along lanes).
-#include <cmath>
-
 #include "fp8_util.h"
 
 namespace mb {
@@ -748,7 +746,7 @@ double tile_cost(int T, int cols, int K, int mb) {
   return 3.5 + (double)((tiles + kComputeUnits - 1) / kComputeUnits) * product;
 }
 // The same in slices of 16 x 16, which come at 30 KB a microsecond and compute unit, and in rings of 32 a x 32 b: rounds, of a start
-// and an end and a block of each wave each (two workgroups of 32 x 32 fit a compute unit).  (Slices, rings of 1 x 1, 1 x 2, 2 x 2,
+// and an end and a block of each wave each.  (Slices, rings of 1 x 1, 1 x 2, 2 x 2,
 // tiles of 64 x 256: 1 x 1024 x 4096 3.5 / 3.8 / 4.4 / 5.4 / 7.7 us, 64 x 4096 x 1024 7.3 / 6.1 / 7.7 / 10.1 / 19.5, 300 x 768 x 768 5.6 / 3.8 / 4.6 /
 // 5.9 / 7.0, 500 x 3072 x 768 20 / 8.3 / 7.4 / 9.1 / 16.8, 685 x 2304 x 768 22 / 9.2 / 10.4 / 8.3 / 12.8, 945 x 768 x 2304 28 / 16 / 17 / 15 / 7.8.)
 double slice_cost(int T, int cols, int K) {
@@ -756,10 +754,11 @@ double slice_cost(int T, int cols, int K) {
   return 2.2 + (double)((groups + kComputeUnits - 1) / kComputeUnits) * (32.0 * K / 30e3);
 }
 double ring_cost(int T, int cols, int K, int a, int b) {
-  const double groups = (double)(((int64_t)T + 32 * a - 1) / (32 * a) * ((cols + 32 * b - 1) / (32 * b))) / kComputeUnits;
+  const int64_t groups = ((int64_t)T + 32 * a - 1) / (32 * a) * ((cols + 32 * b - 1) / (32 * b));
+  const double rounds = (double)((groups + kComputeUnits - 1) / kComputeUnits);
   const int turns = (fp8_blocks(K) + 3) / 4;
-  if (a == 1 && b == 1) return 2.0 + (groups > 1.0 ? groups : 1.0) * (0.9 + 0.4 * turns);
-  return (a == 1 ? 2.2 : 2.5) + std::ceil(groups) * (a == 1 ? 1.4 + 0.6 * turns : 2.4 + 0.8 * turns);
+  if (b == 1) return 2.0 + rounds * (0.9 + 0.38 * turns);
+  return a == 1 ? 2.2 + rounds * (1.4 + 0.6 * turns) : 2.5 + rounds * (2.4 + 0.8 * turns);
 }
 
 // The way with the least estimate, by the sizes alone.

@@ -4,7 +4,9 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import inspect
+import os
 import pickle
+import re
 
 import numpy as np
 import pytest
@@ -12,6 +14,8 @@ import torch
 
 from oracle import fp8_oracle as orc
 from paper_2312_17482_amd import binding as mb
+from paper_2312_17482_amd import build
+from tests.test_lds_load import assembly, too_early
 from tests.test_marshal import STREAM, c_parameters
 
 lib = mb.raw()
@@ -232,6 +236,14 @@ def test_the_calls_pickle_by_name_and_say_what_they_take():
         assert pickle.loads(pickle.dumps(f)) == f
         assert list(inspect.signature(f).parameters) == list(next(a for n, a, _ in all_arguments() if n == name))
         assert f.__doc__
+
+
+def test_no_byte_load_comes_too_early(tmp_path):
+    """Loads of bytes into LDS need the wait states of those of words, in front of them."""
+    code = assembly(os.path.join(build.CSRC, "fp8_gemm.hip"), tmp_path / "code.s")
+    words, _ = too_early(code)
+    loads, found = too_early([re.sub("buffer_load_ubyte (.* lds)$", r"buffer_load_dword \1", l) for l in code])
+    assert loads > words > 0 and not found, found[:10]
 
 
 # ---------------------------------------------------------------------------------------------------- the oracle

@@ -158,7 +158,8 @@ def bound(n, A, fast, y):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("T,n_in,n_out", [(1, 16, 16), (1, 768, 768), (2, 144, 80), (17, 128, 128), (31, 4096, 48), (33, 48, 272),
                                           (64, 256, 256), (65, 272, 144), (129, 768, 144), (257, 1040, 528), (700, 512, 784),
-                                          (1000, 144, 2064), (2500, 768, 768), (4100, 128, 1040)])
+                                          (1000, 144, 2064), (2500, 768, 768), (4100, 128, 1040), (474, 2304, 720), (685, 2320, 784),
+                                          (6200, 144, 3088), (4000, 1024, 4112)])
 def test_linear(T, n_in, n_out, dtype):
     rng = np.random.default_rng(T + n_in + n_out)
     x, xq, xs = stored(rows_of(rng, T, n_in))
@@ -169,21 +170,41 @@ def test_linear(T, n_in, n_out, dtype):
     assert np.linalg.norm(got - y) <= (2.0 ** -8 if dtype == BF16 else 4e-6) * np.linalg.norm(y)
 
 
-def test_linear_strided_result_and_a_row_count_on_the_device():
+@pytest.mark.parametrize("T_cap,n_in,n_out", [(33, 272, 144), (1300, 272, 528), (700, 528, 784), (474, 2304, 720), (685, 2320, 784),
+                                              (2500, 784, 784), (4100, 144, 1040), (6200, 144, 3088), (4000, 1040, 4112),
+                                              (300, 784, 784), (500, 3088, 784), (12000, 144, 2064)])
+def test_linear_strided_result_and_a_row_count_on_the_device(T_cap, n_in, n_out):
     rng = np.random.default_rng(8)
-    T_cap, n_in, n_out = 1300, 272, 528
     x, xq, xs = stored(rows_of(rng, T_cap, n_in))
     w, wq, ws = stored(rng.standard_normal((n_out, n_in)), 128)
     y, A = x @ w.T, np.abs(x) @ np.abs(w).T
     meta = torch.zeros(2, dtype=torch.int32, device="cuda")
     for dtype in (BF16, F32):
-        for T in (0, 1, 64, 65, 300, 1299, 1300, 5000):
+        for T in (0, 1, 65, T_cap - 1, T_cap, T_cap + 3000):
             meta[0] = T
             out = torch.full((T_cap + 3, 2 * n_out), 5.0, dtype=dtype, device="cuda")
             mb.mb_linear_fp8_fwd(xq, xs, wq, ws, meta=meta, y=out[:, n_out:])
             got, n = np64(out), min(T, T_cap)
             assert np.all(np.abs(got[:n, n_out:] - y[:n]) <= bound(n_in, A[:n], dtype == BF16, y[:n]))
             assert np.all(got[n:] == 5.0) and np.all(got[:, :n_out] == 5.0)
+
+
+@pytest.mark.parametrize("T_cap,T,n_out,dtype", [(9000, 8990, 8208, F32), (17000, 16901, 8208, BF16), (17000, 3, 8208, BF16)])
+def test_linear_with_a_result_no_cache_holds(T_cap, T, n_out, dtype):
+    n_in = 48
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    xq, xs = mb.mb_fp8_quant(torch.randn((T_cap, n_in), generator=gen, device="cuda"))
+    wq, ws = mb.mb_fp8_quant_weight(torch.randn((n_out, n_in), generator=gen, device="cuda"), transposed=False)
+    x, w = mb.mb_fp8_dequant(xq, xs, dtype=F32).double(), mb.mb_fp8_dequant(wq, ws.repeat_interleave(128, 0)[:n_out].contiguous(), dtype=F32).double()
+    out = torch.full((T_cap + 1, n_out), 5.0, dtype=dtype, device="cuda")
+    meta = torch.tensor([T, 0], dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        mb.mb_linear_fp8_fwd(xq, xs, wq, ws, meta=meta, y=out[:T_cap])
+    for i in range(0, T, 4096):                      # (in float64 where the results lie, some rows at a time)
+        a, e = x[i:min(i + 4096, T)], out[i:min(i + 4096, T)].double()
+        y, A = a @ w.T, a.abs() @ w.abs().T
+        assert torch.all((e - y).abs() <= bound(n_in, A, False, y) + ((7 * 2.0 ** -13 * A + 2.0 ** -8 * y.abs()) if dtype == BF16 else 0.0))
+    assert torch.all(out[T:] == 5.0)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
@@ -206,7 +227,7 @@ def test_linear_keeps_scales_and_nan_apart(T, dtype):
 
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("T,n_in,n_out", [(1, 16, 16), (5, 144, 80), (63, 128, 272), (64, 256, 256), (65, 1040, 144), (700, 768, 528),
-                                          (4097, 272, 400), (9000, 64, 48)])
+                                          (4097, 272, 400), (9000, 64, 48), (300, 1040, 4112), (6000, 784, 2064), (12000, 528, 528)])
 def test_weight_gradient(T, n_in, n_out, eight):
     rng = np.random.default_rng(T + n_in + n_out)
     x, xq, xs = stored(rows_of(rng, T, n_in))
@@ -250,7 +271,7 @@ def check_eight(q, s, v, err):
 
 
 @pytest.mark.parametrize("T,hidden,inter", [(1, 16, 128), (3, 768, 256), (33, 144, 128), (64, 256, 384), (129, 400, 128),
-                                            (260, 768, 640), (1500, 272, 512), (3000, 128, 1152)])
+                                            (260, 768, 640), (1500, 272, 512), (3000, 128, 1152), (4100, 144, 2176), (8190, 400, 1024)])
 def test_act(T, hidden, inter):
     rng = np.random.default_rng(T + hidden + inter)
     x, xq, xs = stored(rows_of(rng, T, hidden))
@@ -335,15 +356,15 @@ def test_gate_backward(T, inter, eight):
     assert np.abs(diff - slope).max() < 1e-8
 
 
-def test_rows_of_the_gate_behind_the_last_stay():
+@pytest.mark.parametrize("T_cap,T,hidden,inter", [(200, 77, 144, 256), (3000, 2900, 144, 1152), (4100, 257, 144, 2176), (8190, 8001, 400, 1024)])
+def test_rows_of_the_gate_behind_the_last_stay(T_cap, T, hidden, inter):
     rng = np.random.default_rng(3)
-    T_cap, T, hidden, inter = 200, 77, 144, 256
     _, xq, xs = stored(rows_of(rng, T_cap, hidden))
     _, wq, ws = stored(rng.standard_normal((2 * inter, hidden)), 128)
     meta = torch.tensor([T, 0], dtype=torch.int32, device="cuda")
     whole, whole_s = mb.mb_geglu_fp8_act(xq, xs, wq, ws)
     q = torch.full((T_cap, inter), 7.0).to(E4M3).cuda()
-    s = torch.full((T_cap, 2), 99, dtype=torch.uint8).view(E8M0).cuda()
+    s = torch.full((T_cap, inter // 128), 99, dtype=torch.uint8).view(E8M0).cuda()
     mb.mb_geglu_fp8_act(xq, xs, wq, ws, meta=meta, actq=q, acts=s)
     same(val(q)[:T], val(whole)[:T])
     same(exps(s)[:T], exps(whole_s)[:T])
@@ -351,7 +372,7 @@ def test_rows_of_the_gate_behind_the_last_stay():
     da, hg = dev(rows_of(rng, T_cap, inter), BF16), dev(rng.standard_normal((T_cap, 2 * inter)), BF16)
     whole, whole_s = mb.mb_gelu_gate_fp8_bwd(da, hg)
     q = torch.full((T_cap, 2 * inter), 7.0).to(E4M3).cuda()
-    s = torch.full((T_cap, 4), 99, dtype=torch.uint8).view(E8M0).cuda()
+    s = torch.full((T_cap, inter // 64), 99, dtype=torch.uint8).view(E8M0).cuda()
     mb.mb_gelu_gate_fp8_bwd(da, hg, meta=meta, dhgq=q, dhgs=s)
     same(val(q)[:T], val(whole)[:T])
     same(exps(s)[:T], exps(whole_s)[:T])
