@@ -366,7 +366,8 @@ MB_API mb_status mb_gelu_gate(const void* h, const void* gate, int64_t row_strid
  *   Storing a block takes the smallest scale 2^e, e >= -126, with every finite |x| <= 448 * 2^e, and rounds x / 2^e to the nearest
  *   e4m3 value (ties to even).  Infinities and NaN are stored as NaN and have no part in the scale.  A block of zeros has b = 1.
  * T_cap, meta_dev: rows [0, T), T = min(meta_dev[0], T_cap) or T_cap if meta_dev is NULL; the others are neither read nor
- * written.  Limits: T_cap <= 2^30, T_cap * W < 2^35, row strides < 2^21 elements and a multiple of 16 bytes (MB_ERR_UNSUPPORTED, MB_ERR_INVALID_ARG).
+ * written.  Limits: T_cap <= 2^30, T_cap * W < 2^35 in less than 2^29 blocks, row strides < 2^21 elements (MB_ERR_UNSUPPORTED) and a
+ * multiple of 16 bytes (MB_ERR_INVALID_ARG).
  *
  * mb_fp8_quant         x [T_cap, W] of row stride x_row_stride (elements), dt -> q, s.
  * mb_fp8_dequant       q, s -> x, rounded once to dt.
@@ -399,6 +400,7 @@ MB_API mb_status mb_linear_fp8_fwd(const uint8_t* xq, const uint8_t* xs, const u
  *   dw       dev, [n_out, n_in] float, written (zeros if T = 0).
  *   workspace  dev, at least mb_linear_fp8_wgrad_workspace_bytes bytes, scratch; may be NULL if that is 0.
  * Deterministic: sums over tokens are taken in a fixed order that depends on the sizes (T_cap among them) only.
+ * n_in * n_out < 2^31 (MB_ERR_UNSUPPORTED).
  */
 MB_API size_t mb_linear_fp8_wgrad_workspace_bytes(int T_cap, int n_in, int n_out);
 MB_API mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy_row_stride, const uint8_t* xq,

@@ -38,9 +38,10 @@ mb_status check_stride(int64_t stride, int W, mb_dtype dt, const char* name) {
     if (st_ != MB_OK) return st_;     \
   } while (0)
 
-// (the row kernels count a row's pieces of 16 in 32 bits)
+// (the row kernels count a row's pieces of 16 in 32 bits, and a launch has less than 2^32 threads: 8 to a block)
 mb_status check_matrix(int T_cap, int W) {
   MB_REQUIRE((int64_t)T_cap * W < ((int64_t)1 << 35), MB_ERR_UNSUPPORTED, "matrix of 2^35 elements or more (%d x %d)", T_cap, W);
+  MB_REQUIRE((int64_t)T_cap * ((W + 127) / 128) < ((int64_t)1 << 29), MB_ERR_UNSUPPORTED, "2^29 blocks of 128 or more (%d x %d)", T_cap, W);
   return MB_OK;
 }
 mb_status check_product(int T_cap, int n_in, int n_out) {
@@ -48,6 +49,12 @@ mb_status check_product(int T_cap, int n_in, int n_out) {
   MB_CHECK(check_width(n_in, 16, "n_in"));
   MB_CHECK(check_width(n_out, 16, "n_out"));
   MB_REQUIRE((int64_t)T_cap * n_out < ((int64_t)1 << 38), MB_ERR_UNSUPPORTED, "T_cap * n_out of 2^38 or more (%d, %d)", T_cap, n_out);
+  return MB_OK;
+}
+// (partial gradients are added up by two threads for an element at most, of less than 2^32 in a launch)
+mb_status check_gradient(int T_cap, int n_in, int n_out) {
+  MB_CHECK(check_product(T_cap, n_in, n_out));
+  MB_REQUIRE((int64_t)n_in * n_out < ((int64_t)1 << 31), MB_ERR_UNSUPPORTED, "gradient of 2^31 elements or more (%d x %d)", n_out, n_in);
   return MB_OK;
 }
 
@@ -119,7 +126,7 @@ mb_status mb_linear_fp8_fwd(const uint8_t* xq, const uint8_t* xs, const uint8_t*
 }
 
 size_t mb_linear_fp8_wgrad_workspace_bytes(int T_cap, int n_in, int n_out) {
-  if (check_product(T_cap, n_in, n_out) != MB_OK) return 0;
+  if (check_gradient(T_cap, n_in, n_out) != MB_OK) return 0;
   return linear_fp8_wgrad_workspace_bytes(T_cap, n_in, n_out);
 }
 
@@ -127,7 +134,7 @@ mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t dy_row
                               int T_cap, const int32_t* meta_dev, int n_in, int n_out, float* dw, void* workspace,
                               size_t workspace_bytes, void* stream) {
   clear_error();
-  MB_CHECK(check_product(T_cap, n_in, n_out));
+  MB_CHECK(check_gradient(T_cap, n_in, n_out));
   if (dys == nullptr) MB_CHECK(check_stride(dy_row_stride, n_out, MB_BF16, "dy_row_stride"));
   else MB_REQUIRE(dy_row_stride == n_out, MB_ERR_INVALID_ARG, "8-bit rows of dy are contiguous: dy_row_stride=%lld, n_out=%d",
                   (long long)dy_row_stride, n_out);

@@ -104,29 +104,33 @@ __device__ __forceinline__ double gated_value64(const Product& pr, int row, int 
   return gelu64(h) * sum;
 }
 
-// LDS of a tile shape, bytes: stages of 64 kMB token rows and 32 kWN kNB weight rows, a word for each of 64 scales per wave
-// and stage; the waves' slabs of 32 x 64 bytes for the way out, or the largest magnitudes of a tile's tokens by wave (kAct).
-template <int kMB, int kWN, int kNB>
-constexpr int kStageBytes = (64 * kMB + 32 * kWN * kNB) * kStep + 2 * kWN * 256;
-template <int kMB, int kWN, int kNB, int kStages>
-constexpr int kLdsBytes = kStages * kStageBytes<kMB, kWN, kNB> + 2 * kWN * 2048;
+constexpr int kWN = 4, kNB = 2;     // waves along the weight rows, and their blocks of 32
+constexpr int kBN = 32 * kWN * kNB, kWaves = 2 * kWN;
+constexpr int kDepth = 2;           // buffers that token fragments rotate through
 
-// Workgroup of 2 kWN waves (2 along the tokens by kWN along the weight rows): tiles blockIdx.x, + gridDim.x, ... of 64 kMB tokens
-// x 32 kWN kNB weight rows; a wave computes 32 kMB x 32 kNB.  Token fragments rotate through kDepth buffers.
+// Stages of a tile of 64 mb tokens (as many as fit), and LDS in bytes: stages of 64 mb token rows and 256 weight rows, a word for
+// each of 64 scales per wave and stage; the waves' slabs of 32 x 64 bytes for the way out, or the largest magnitudes of a tile's
+// tokens by wave (kAct).
+constexpr int stages_of(int mb) { return mb == 1 ? 3 : 2; }
+constexpr int stage_bytes(int mb) { return (64 * mb + kBN) * kStep + kWaves * 256; }
+constexpr int lds_bytes(int mb) { return stages_of(mb) * stage_bytes(mb) + kWaves * 2048; }
+
+// Workgroup of 8 waves (2 along the tokens by 4 along the weight rows): tiles blockIdx.x, + gridDim.x, ... of 64 kMB tokens
+// x 256 weight rows; a wave computes 32 kMB x 64.
 //
 // Stages free up in two halves where that can be had (kTwice: 256 tokens).  A step is eight slots of two matrix instructions, a
 // slot a block of 32 tokens and a half of the step's k; the slots of blocks 0 and 1 come first.  By the middle of the step
 // every wave has read all of the weight and these blocks, and a barrier there lets their places be requested for the step after
 // next; those of blocks 2 and 3 follow at the end.  So everything is requested one and a half steps before it is needed, with
 // two stages: a step's 64 KB take 1.2 to 1.5 us to come when requested at once, its matrix instructions 1.0 us.
-template <int kMode, int kMB, int kWN, int kNB, int kStages, int kDepth>
+template <int kMode, int kMB>
 __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __restrict__ smem, int wave) {
   constexpr bool kGated = kMode == kAct, kExact = is_exact(kMode);
-  constexpr bool kTwice = kMB == 4 && kWN == 4 && kStages == 2 && kDepth == 2;
-  constexpr int kBM = 64 * kMB, kBN = 32 * kWN * kNB, kWaves = 2 * kWN;
-  static_assert(!kGated || (kNB == 2 && kBN == 256), "the gate pairs the wave's two weight blocks; 128 columns are a block");
+  constexpr bool kTwice = kMB == 4;
+  constexpr int kBM = 64 * kMB, kStages = stages_of(kMB);
+  static_assert(kNB == 2 && kBN == 256, "the gate pairs the wave's two weight blocks; 128 columns are a block");
   constexpr int kRows = kBM + kBN;
-  constexpr int kStage = kStageBytes<kMB, kWN, kNB>;
+  constexpr int kStage = stage_bytes(kMB);
   constexpr int kScales = kRows * kStep;             // offset of the scales in a stage
   constexpr int kLoads = kRows / (8 * kWaves);       // 8-row loads per wave and step
   constexpr int kSlots = 2 * kMB;                    // a step: two halves of 64 k, a slot for each block of 32 tokens
@@ -481,18 +485,19 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
   stage_ready<0>();   // no load may still be on its way to LDS that the next workgroup owns
 }
 
-template <int kMode, int kMB, int kWN, int kNB, int kStages, int kDepth>
-__global__ __launch_bounds__(128 * kWN, kWN / 2) void fp8_gemm_kernel(Product pr) {
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kLdsBytes<kMB, kWN, kNB, kStages>];
+template <int kMode, int kMB>
+__global__ __launch_bounds__(64 * kWaves, 2) void fp8_gemm_kernel(Product pr) {
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[lds_bytes(kMB)];
   const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
-  fp8_tiles<kMode, kMB, kWN, kNB, kStages, kDepth>(pr, T, smem, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  fp8_tiles<kMode, kMB>(pr, T, smem, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
-// Products of a few rows, whose time is that of the way to memory and back: 16 kA tokens x 16 kB columns by 8 waves that share the
+// Products of a few rows, whose time is that of the way to memory and back: 16 tokens x 16 columns by 8 waves that share the
 // contraction, wave w its blocks w, w + 8, ... of 128 k.  No stages and no barrier in it: a wave requests a block's rows straight
 // into the registers the matrix instruction reads (v_mfma_scale_f32_16x16x128_f8f6f4, one a block; exact: four of
 // v_mfma_f32_16x16x32_bf16), the next block's while it multiplies, and the waves' sums meet in LDS once, added in order.
-constexpr int kSliceWaves = 8;
+// (1 x 768 x 768: 3.0 us.)
+constexpr int kSliceWaves = 8, kSlice = 16;
 
 // Where piece p (4 columns) of token t's sums lies: the pieces of neighbouring tokens in different banks.
 template <int kPieces>
@@ -513,69 +518,51 @@ __device__ __forceinline__ void store_sums(const Product& pr, const float* sums,
   }
 }
 
-template <int kMode, int kA, int kB>
+template <int kMode>
 __global__ __launch_bounds__(64 * kSliceWaves) void fp8_slice_kernel(Product pr) {
-  constexpr bool kExact = is_exact(kMode);
-  constexpr int kTM = 16 * kA, kTN = 16 * kB, kPieces = kTN / 4;   // 16-byte pieces of a token's sums
-  __shared__ __attribute__((aligned(16))) float sums[kSliceWaves * kTM * kTN];
+  constexpr int kPieces = kSlice / 4;   // 16-byte pieces of a token's sums
+  __shared__ __attribute__((aligned(16))) float sums[kSliceWaves * kSlice * kSlice];
   const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
-  const int m0 = blockIdx.y * kTM, n0 = blockIdx.x * kTN;
+  const int m0 = blockIdx.y * kSlice, n0 = blockIdx.x * kSlice;
   if (m0 >= T) return;
-  const int K = pr.K, blocks = fp8_blocks(K), w_rows = pr.w_rows;
+  const int K = pr.K, blocks = fp8_blocks(K);
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int xrows = min(T - m0, kTM), wrows = min(w_rows - n0, kTN);
+  const int xrows = min(T - m0, kSlice), wrows = min(pr.w_rows - n0, kSlice);
   const __amdgpu_buffer_rsrc_t xr = uniform_rsrc(pr.x + (int64_t)m0 * K, (uint32_t)xrows * (uint32_t)K);
   const __amdgpu_buffer_rsrc_t wr = uniform_rsrc(pr.w + (int64_t)n0 * K, (uint32_t)wrows * (uint32_t)K);
   const __amdgpu_buffer_rsrc_t xsr = uniform_rsrc(pr.xs + (int64_t)m0 * blocks, (uint32_t)xrows * (uint32_t)blocks);
-  const __amdgpu_buffer_rsrc_t wsr = uniform_rsrc(pr.ws, (uint32_t)fp8_blocks(w_rows) * (uint32_t)blocks);
+  const __amdgpu_buffer_rsrc_t wsr = uniform_rsrc(pr.ws + (int64_t)(n0 / kFp8Block) * blocks, (uint32_t)blocks);
   // A lane's 32 bytes of a row: pieces g and g + 4 (four lanes request 64 bytes in one go).  Rows and pieces that do not
   // exist are out of the descriptor's range and zeros.
   struct Block {
-    i32x8 x[kA], w[kB];
-    uint32_t xs[kA], ws[kB];
+    i32x8 x, w;
+    uint32_t xs, ws;
   };
   auto request = [&](Block& b, int kb) {
-    auto rows = [&](i32x8& r, __amdgpu_buffer_rsrc_t from, int row) {
+    auto rows = [&](i32x8& r, __amdgpu_buffer_rsrc_t from) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const int k = kb * kFp8Block + (g + 4 * u) * 16;
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, k < K ? (uint32_t)row * (uint32_t)K + k : 0x80000000u, 0, 0);
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, k < K ? (uint32_t)c * (uint32_t)K + k : 0x80000000u, 0, 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) r[4 * u + i] = (int)v[i];
       }
     };
-#pragma unroll
-    for (int i = 0; i < kB; ++i) rows(b.w[i], wr, 16 * i + c);
-#pragma unroll
-    for (int i = 0; i < kA; ++i) rows(b.x[i], xr, 16 * i + c);
-#pragma unroll
-    for (int i = 0; i < kB; ++i)
-      b.ws[i] = __builtin_amdgcn_raw_buffer_load_b8(wsr, (uint32_t)((n0 + 16 * i) / kFp8Block) * (uint32_t)blocks + kb, 0, 0);
-#pragma unroll
-    for (int i = 0; i < kA; ++i) b.xs[i] = __builtin_amdgcn_raw_buffer_load_b8(xsr, (uint32_t)(16 * i + c) * (uint32_t)blocks + kb, 0, 0);
+    rows(b.w, wr);
+    rows(b.x, xr);
+    b.ws = __builtin_amdgcn_raw_buffer_load_b8(wsr, kb, 0, 0);
+    b.xs = __builtin_amdgcn_raw_buffer_load_b8(xsr, (uint32_t)c * (uint32_t)blocks + kb, 0, 0);
   };
-  f32x4 acc[kA][kB] = {};
+  f32x4 acc = {};
   auto multiply = [&](const Block& b) {
-    if constexpr (kExact) {
+    if constexpr (is_exact(kMode)) {
 #pragma unroll
-      for (int p = 0; p < 4; ++p) {
-        bf16x8 xb[kA];
-#pragma unroll
-        for (int i = 0; i < kA; ++i) xb[i] = to_bf16x8(b.x[i][2 * p], b.x[i][2 * p + 1], __uint_as_float(b.xs[i] << 23));
-#pragma unroll
-        for (int j = 0; j < kB; ++j) {
-          const bf16x8 wb = to_bf16x8(b.w[j][2 * p], b.w[j][2 * p + 1], __uint_as_float(b.ws[j] << 23));
-#pragma unroll
-          for (int i = 0; i < kA; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb, xb[i], acc[i][j], 0, 0, 0);
-        }
-      }
+      for (int p = 0; p < 4; ++p)
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(to_bf16x8(b.w[2 * p], b.w[2 * p + 1], scale_bits(b.ws)),
+                                                      to_bf16x8(b.x[2 * p], b.x[2 * p + 1], scale_bits(b.xs)), acc, 0, 0, 0);
     } else {
-#pragma unroll
-      for (int j = 0; j < kB; ++j)
-#pragma unroll
-        for (int i = 0; i < kA; ++i)
-          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.w[j], b.x[i], acc[i][j], 0, 0, 0, (int)b.ws[j], 0, (int)b.xs[i]);
+      acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(b.w, b.x, acc, 0, 0, 0, (int)b.ws, 0, (int)b.xs);
     }
   };
   Block now, ahead;
@@ -587,29 +574,24 @@ __global__ __launch_bounds__(64 * kSliceWaves) void fp8_slice_kernel(Product pr)
     if (kb + 2 * kSliceWaves < blocks) request(now, kb + 2 * kSliceWaves);
     multiply(ahead);
   }
-  // Lane (c, g) holds columns 16 j + 4 g .. + 3 of token 16 i + c.
-  if (wave < blocks) {
-#pragma unroll
-    for (int i = 0; i < kA; ++i)
-#pragma unroll
-      for (int j = 0; j < kB; ++j)
-        *reinterpret_cast<f32x4*>(&sums[wave * kTM * kTN + sum_place<kPieces>(16 * i + c, 4 * j + g)]) = acc[i][j];
-  }
+  // Lane (c, g) holds columns 4 g .. + 3 of token c.
+  if (wave < blocks) *reinterpret_cast<f32x4*>(&sums[wave * kSlice * kSlice + sum_place<kPieces>(c, g)]) = acc;
   __syncthreads();
-  store_sums<kMode, kTM, kTN, 64 * kSliceWaves>(pr, sums, min(blocks, kSliceWaves), m0, n0, T);
+  store_sums<kMode, kSlice, kSlice, 64 * kSliceWaves>(pr, sums, min(blocks, kSliceWaves), m0, n0, T);
 }
 
 // The same with the operands' way through LDS, for products of some hundred rows, where the direct way's 64 bytes of a row at a
-// time are the bound (14 bytes a cycle and compute unit): 32 kA tokens x 32 kB columns by kW waves, each with two stages of its
+// time are the bound (14 bytes a cycle and compute unit): 32 kA tokens x 32 kB columns by 4 waves, each with two stages of its
 // own that it fills itself by whole 128-byte lines.  A wave waits for its own loads only; no barrier until the sums meet.
-template <int kMode, int kA, int kB, int kW>
-__global__ __launch_bounds__(64 * kW) void fp8_ring_kernel(Product pr) {
+constexpr int kRingWaves = 4;
+template <int kMode, int kA, int kB>
+__global__ __launch_bounds__(64 * kRingWaves) void fp8_ring_kernel(Product pr) {
   constexpr bool kExact = is_exact(kMode);
   constexpr int kTM = 32 * kA, kTN = 32 * kB, kPieces = kTN / 4, kRows = kTM + kTN;
   constexpr int kStage = kRows * kStep + 512;      // rows, 64 words of token scales, 64 of the weight's (all alike)
   constexpr int kLoads = kRows / 8 + 2;
   static_assert(kTM <= 64 && kTN <= 128 && 2 * kStage >= kTM * kTN * 4, "one load brings the scales; the sums take the stages' place");
-  __shared__ __attribute__((aligned(1024))) uint8_t smem[kW * 2 * kStage];
+  __shared__ __attribute__((aligned(1024))) uint8_t smem[kRingWaves * 2 * kStage];
   const int T = __builtin_amdgcn_readfirstlane(pr.meta ? min(pr.meta[0], pr.T_cap) : pr.T_cap);
   const int m0 = blockIdx.y * kTM, n0 = blockIdx.x * kTN;
   if (m0 >= T) return;
@@ -643,11 +625,11 @@ __global__ __launch_bounds__(64 * kW) void fp8_ring_kernel(Product pr) {
   f32x16 acc[kA][kB] = {};
   if (wave < blocks) {
     fetch(wave, 0);
-    if (wave + kW >= blocks) xr[2] = wr[2] = xsr[2] = wsr[2] = 0u;   // (past the end the loads bring nothing; their number stays)
-    fetch(wave + kW, 1);
+    if (wave + kRingWaves >= blocks) xr[2] = wr[2] = xsr[2] = wsr[2] = 0u;   // (past the end the loads bring nothing; their number stays)
+    fetch(wave + kRingWaves, 1);
     int stage = 0;
 #pragma unroll 1
-    for (int kb = wave; kb < blocks; kb += kW) {
+    for (int kb = wave; kb < blocks; kb += kRingWaves) {
       asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLoads) : "memory");
       const uint8_t* const from = smem + wave * (2 * kStage) + stage * kStage;
       i32x8 f[2][kA + kB];
@@ -669,8 +651,8 @@ __global__ __launch_bounds__(64 * kW) void fp8_ring_kernel(Product pr) {
       for (int i = 0; i < kA; ++i) sx[i] = sc[32 * i + c];
       const uint32_t sw = sc[64];
       asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");   // (read: the stage may be filled again)
-      if (kb + 2 * kW >= blocks) xr[2] = wr[2] = xsr[2] = wsr[2] = 0u;
-      fetch(kb + 2 * kW, stage);
+      if (kb + 2 * kRingWaves >= blocks) xr[2] = wr[2] = xsr[2] = wsr[2] = 0u;
+      fetch(kb + 2 * kRingWaves, stage);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         if constexpr (kExact) {
@@ -710,28 +692,26 @@ __global__ __launch_bounds__(64 * kW) void fp8_ring_kernel(Product pr) {
               f32x4{acc[i][j][4 * v], acc[i][j][4 * v + 1], acc[i][j][4 * v + 2], acc[i][j][4 * v + 3]};
   }
   __syncthreads();
-  store_sums<kMode, kTM, kTN, 64 * kW>(pr, sums, min(blocks, kW), m0, n0, T);
-}
-
-template <int kMode, int kA, int kB, int kW>
-void launch_rings(const Product& pr, hipStream_t stream) {
-  const dim3 grid((pr.w_rows + 32 * kB - 1) / (32 * kB), (pr.T_cap + 32 * kA - 1) / (32 * kA));
-  fp8_ring_kernel<kMode, kA, kB, kW><<<grid, dim3(64 * kW), 0, stream>>>(pr);
+  store_sums<kMode, kTM, kTN, 64 * kRingWaves>(pr, sums, min(blocks, kRingWaves), m0, n0, T);
 }
 
 template <int kMode, int kA, int kB>
-void launch_slices(const Product& pr, hipStream_t stream) {
-  const dim3 grid((pr.w_rows + 16 * kB - 1) / (16 * kB), (pr.T_cap + 16 * kA - 1) / (16 * kA));
-  fp8_slice_kernel<kMode, kA, kB><<<grid, dim3(64 * kSliceWaves), 0, stream>>>(pr);
+void launch_rings(const Product& pr, hipStream_t stream) {
+  const dim3 grid((pr.w_rows + 32 * kB - 1) / (32 * kB), (pr.T_cap + 32 * kA - 1) / (32 * kA));
+  fp8_ring_kernel<kMode, kA, kB><<<grid, dim3(64 * kRingWaves), 0, stream>>>(pr);
 }
 
-template <int kMode, int kMB, int kWN, int kNB, int kStages, int kDepth>
+template <int kMode>
+void launch_slices(const Product& pr, hipStream_t stream) {
+  const dim3 grid((pr.w_rows + kSlice - 1) / kSlice, (pr.T_cap + kSlice - 1) / kSlice);
+  fp8_slice_kernel<kMode><<<grid, dim3(64 * kSliceWaves), 0, stream>>>(pr);
+}
+
+template <int kMode, int kMB>
 void launch_tiles(Product pr, int cols, hipStream_t stream) {
-  constexpr int kBN = 32 * kWN * kNB;
   pr.n_tiles = (cols + kBN - 1) / kBN;
   const int64_t total = (int64_t)((pr.T_cap + 64 * kMB - 1) / (64 * kMB)) * pr.n_tiles;
-  fp8_gemm_kernel<kMode, kMB, kWN, kNB, kStages, kDepth>
-      <<<dim3((unsigned)(total < kComputeUnits ? total : kComputeUnits)), dim3(128 * kWN), 0, stream>>>(pr);
+  fp8_gemm_kernel<kMode, kMB><<<dim3((unsigned)(total < kComputeUnits ? total : kComputeUnits)), dim3(64 * kWaves), 0, stream>>>(pr);
 }
 
 // Estimated microseconds in tiles of 64 `mb` tokens: rounds over the compute units, a step and a tile's start and end each.
@@ -746,9 +726,9 @@ double tile_cost(int T, int cols, int K, int mb) {
   return 3.5 + (double)((tiles + kComputeUnits - 1) / kComputeUnits) * product;
 }
 // The same in slices of 16 x 16, which come at 30 KB a microsecond and compute unit, and in rings of 32 a x 32 b: rounds, of a start
-// and an end and a block of each wave each.  (Slices, rings of 1 x 1, 1 x 2, 2 x 2,
-// tiles of 64 x 256: 1 x 1024 x 4096 3.5 / 3.8 / 4.4 / 5.4 / 7.7 us, 64 x 4096 x 1024 7.3 / 6.1 / 7.7 / 10.1 / 19.5, 300 x 768 x 768 5.6 / 3.8 / 4.6 /
-// 5.9 / 7.0, 500 x 3072 x 768 20 / 8.3 / 7.4 / 9.1 / 16.8, 685 x 2304 x 768 22 / 9.2 / 10.4 / 8.3 / 12.8, 945 x 768 x 2304 28 / 16 / 17 / 15 / 7.8.)
+// and an end and a block of each wave each.  (Slices, rings of 1 x 1, 1 x 2, 2 x 2, tiles of 64 x 256: 1 x 1024 x 4096 3.5 / 3.8 /
+// 4.4 / 5.4 / 7.7 us, 64 x 4096 x 1024 7.3 / 6.1 / 7.7 / 10.1 / 19.5, 300 x 768 x 768 5.6 / 3.8 / 4.6 / 5.9 / 7.0, 500 x 3072 x 768
+// 20 / 8.3 / 7.4 / 9.1 / 16.8, 685 x 2304 x 768 22 / 9.2 / 10.4 / 8.3 / 12.8, 945 x 768 x 2304 28 / 16 / 17 / 15 / 7.8.)
 double slice_cost(int T, int cols, int K) {
   const int64_t groups = ((int64_t)T + 15) / 16 * ((cols + 15) / 16);
   return 2.2 + (double)((groups + kComputeUnits - 1) / kComputeUnits) * (32.0 * K / 30e3);
@@ -782,19 +762,19 @@ void launch_product(const Product& pr, int cols, hipStream_t stream) {
       offer(264, ring_cost(T, cols, K, 2, 2));
     }
     switch (best) {
-      case 11: return launch_slices<kMode, 1, 1>(pr, stream);
-      case 132: return launch_rings<kMode, 1, 1, 4>(pr, stream);
-      case 164: return launch_rings<kMode, 1, 2, 4>(pr, stream);
-      case 264: return launch_rings<kMode, 2, 2, 4>(pr, stream);
+      case 11: return launch_slices<kMode>(pr, stream);
+      case 132: return launch_rings<kMode, 1, 1>(pr, stream);
+      case 164: return launch_rings<kMode, 1, 2>(pr, stream);
+      case 264: return launch_rings<kMode, 2, 2>(pr, stream);
       default: break;
     }
   }
   switch (best) {
-    case 1: return launch_tiles<kMode, 1, 4, 2, 3, 2>(pr, cols, stream);
-    case 2: return launch_tiles<kMode, 2, 4, 2, 2, 2>(pr, cols, stream);
-    case 3: return launch_tiles<kMode, 3, 4, 2, 2, 2>(pr, cols, stream);
+    case 1: return launch_tiles<kMode, 1>(pr, cols, stream);
+    case 2: return launch_tiles<kMode, 2>(pr, cols, stream);
+    case 3: return launch_tiles<kMode, 3>(pr, cols, stream);
     default:
-      if constexpr (!is_exact(kMode)) launch_tiles<kMode, 4, 4, 2, 2, 2>(pr, cols, stream);
+      if constexpr (!is_exact(kMode)) launch_tiles<kMode, 4>(pr, cols, stream);
   }
 }
 

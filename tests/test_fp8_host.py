@@ -55,6 +55,8 @@ REFUSED = [
     ("mb_linear_fp8_wgrad", dict(dys=A, dy_row_stride=96), BAD, "contiguous"), ("mb_linear_fp8_wgrad", dict(dys=A + 2), BAD, "dys is not"),
     ("mb_linear_fp8_wgrad", dict(dy_row_stride=72), BAD, "dy_row_stride"), ("mb_linear_fp8_wgrad", dict(xq=None), BAD, "xq is NULL"),
     ("mb_linear_fp8_wgrad", dict(T_cap=27000), mb.MB_ERR_WORKSPACE, "needed"),
+    ("mb_fp8_quant", dict(T_cap=1 << 29, W=16, x_row_stride=16), NOT, "2^29"), ("mb_fp8_dequant", dict(T_cap=1 << 30, W=16, x_row_stride=16), NOT, "2^29"),
+    ("mb_linear_fp8_wgrad", dict(n_in=1 << 16, n_out=1 << 15, dy_row_stride=1 << 15), NOT, "gradient of 2^31"),
     ("mb_linear_fp8_wgrad", dict(T_cap=27000, workspace=A + 8, workspace_bytes=1 << 30), BAD, "workspace is not"),
     ("mb_geglu_fp8_act", dict(inter=192), NOT, "multiple of 128"), ("mb_geglu_fp8_act", dict(hidden=8), NOT, "hidden"),
     ("mb_geglu_fp8_act", dict(hidden=1 << 16, inter=1 << 16), NOT, "2^31"), ("mb_geglu_fp8_act", dict(acts=None), BAD, "acts is NULL"),
