@@ -114,12 +114,25 @@ __device__ __forceinline__ float normal_tail(float h, float& e) {
   e = __builtin_amdgcn_exp2f(h * (h * (-0.5f * kLog2e)));
   return p * t * e;
 }
-// GeLU(h) = h Phi(h) = max(h, 0) - |h| Phi(-|h|), and with its derivative Phi(h) + h phi(h).
+// GeLU(h) = h Phi(h) = max(h, 0) - |h| Phi(-|h|) alone, where the derivative's exp(-h^2 / 2) is not needed as well: Phi(-|h|) as
+// 2^Q(|h|), Q of degree 9 fitted for the least error over |h| = 0 .. 13.4, 2.4e-5 of the value (with fp32's rounding 3.4e-5 up to
+// 11 and 4.5e-5 beyond).  One transcendental instead of two, which take as long as four other instructions each.  (Q falls
+// on beyond the fit.)
 __device__ __forceinline__ float gelu_tail(float h) {
-  float e;
-  const float u = normal_tail(h, e);
-  return fmaf(-fabsf(h), u, fmaxf(h, 0.0f));
+  const float x = fabsf(h);
+  float q = fmaf(-1.8374048948999189e-09f, x, 1.3548363142490416e-07f);
+  q = fmaf(q, x, -4.38907682109857e-06f);
+  q = fmaf(q, x, 8.267235534731299e-05f);
+  q = fmaf(q, x, -0.001013598870486021f);
+  q = fmaf(q, x, 0.008634578436613083f);
+  q = fmaf(q, x, -0.053876444697380066f);
+  q = fmaf(q, x, -0.45889127254486084f);
+  q = fmaf(q, x, -1.1509331464767456f);
+  q = fmaf(q, x, -1.0000337362289429f);
+  const float above = __uint_as_float((uint32_t)max((int)__float_as_uint(h), 0));   // max(h, 0), without quieting a NaN first
+  return fmaf(-x, __builtin_amdgcn_exp2f(q), above);
 }
+// The same and the derivative Phi(h) + h phi(h).
 __device__ __forceinline__ void gelu_tail_and_grad(float h, float& val, float& grad) {
   float e;
   const float u = normal_tail(h, e);
