@@ -25,9 +25,10 @@ struct Wgrad {
   float* out;                     // of the first split; split s is n_out n_in floats further on, s times
 };
 
-// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4) ^ 2 (r % 2) ^ x / 16 % 2.  The four rows a transposing read
-// touches lie in different banks, and so do the pieces that 16 lanes, 8 of a row, write at a time of their 32 bytes in 8 bits.
-__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ (2 * (r & 1)) ^ (x >> 4 & 1); }
+// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4) ^ x / 8 % 4.  The four rows a transposing read touches lie in
+// different banks (of 64), and the pieces that 8 lanes of a row write at a time, every second or fourth one, in different
+// banks of the 32 that a write sees.
+__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ (x >> 3 & 3); }
 
 // The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.  In 8 bits a thread takes 16 or 32
 // bytes of one row, which have one scale (a load of its own for each 16 bytes took a tenth of the whole time).
@@ -228,8 +229,9 @@ __global__ __launch_bounds__(512, 4) void fp8_wgrad_slice_kernel(Wgrad pr) {
   const int tile = blockIdx.x, tile_m = tile / pr.n_tiles;
   const int m0 = tile_m * 64, n0 = (tile - tile_m * pr.n_tiles) * 64;
   uint16_t* const area = smem + wave * kArea;
-  // Piece x (8 columns) of row r at position x ^ 5 (r / 2 % 2): four rows' reads, and the writes of 16 lanes, in different banks.
-  auto place = [](int x, int r) { return r * 64 + ((x ^ (5 * (r >> 1 & 1))) * 8); };
+  // Piece x (8 columns) of row r at position x ^ r % 2 ^ 4 (r / 2 % 2): four rows' reads in different banks of 64, and the writes of
+  // 8 lanes, every second piece of two rows, in different ones of 32.
+  auto place = [](int x, int r) { return r * 64 + ((x ^ (r & 1) ^ (4 * (r >> 1 & 1))) * 8); };
   constexpr int kPer = kEight ? 4 : 8, kP = kChunk * kPer / 64, kQ = kChunk * 4 / 64;   // lanes per row of dy, loads of dy and x
   const int64_t ppitch = pr.dy_stride * (kEight ? 1 : 2);
   const int blocks_p = fp8_blocks(pr.n_out), blocks_q = fp8_blocks(pr.n_in);
