@@ -25,13 +25,13 @@ struct Wgrad {
   float* out;                     // of the first split; split s is n_out n_in floats further on, s times
 };
 
-// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4) ^ x / 8 % 4.  The four rows a transposing read touches lie in
-// different banks (of 64), and the pieces that 8 lanes of a row write at a time, every second or fourth one, in different
-// banks of the 32 that a write sees.
-__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ (x >> 3 & 3); }
+// Piece x (8 bf16 columns) of row r sits at position x ^ 4 (r % 4) ^ (x / 8 + x / 16) % 2.  The four rows a transposing read touches
+// lie in different banks (of 64), and so do the pieces that 8 lanes of a row write at a time, every second one of 8 or 16 and
+// of another 8, in the 32 banks that a write sees.
+__device__ __forceinline__ int place_of(int x, int r) { return x ^ (4 * (r & 3)) ^ ((x >> 3 ^ x >> 4) & 1); }
 
-// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.  In 8 bits a thread takes 16 or 32
-// bytes of one row, which have one scale (a load of its own for each 16 bytes took a tenth of the whole time).
+// The rows of one operand on their way into LDS: kCols columns of 64 tokens, 512 threads.  In 8 bits a thread takes 16 bytes of one
+// row, or 16 and those 64 further on, which have one scale (a load of its own for each 16 bytes took a tenth of the whole time).
 template <bool kEight, int kCols>
 struct Stager {
   static constexpr int kPieces = kCols / (kEight ? 16 : 8);   // 16-byte pieces of a row in memory
@@ -39,21 +39,21 @@ struct Stager {
   static constexpr int kLanes = kEight ? 8 : kPieces;         // threads per row
   u32x4 data[kN];
   uint32_t byte;
-  int row, piece;           // of the first; the n-th is the next piece (8 bits), or lies 512 / kLanes rows on
+  int row, piece;           // of the first; the n-th lies 4 pieces on (8 bits), or 512 / kLanes rows
   uint32_t off, soff;       // byte offsets in a step's rows
-  int there;                // pieces that are columns
+  int there;                // bytes from here to the row's end
   const uint8_t *base, *sbase;
   int64_t pitch;            // bytes from row to row
   int blocks, T;
   __device__ __forceinline__ Stager(const void* p, const uint8_t* s, int64_t stride, int first_col, int cols, int T_, int tid) {
     constexpr int kEs = kEight ? 1 : 2;
     row = tid / kLanes;
-    piece = tid % kLanes * (kEight ? kN : 1);
+    piece = tid % kLanes + (kEight && kN == 2 ? tid & 4 : 0);   // (4 lanes request 64 bytes in one go)
     pitch = stride * kEs;
     blocks = fp8_blocks(cols);
     T = T_;
     const int col = first_col + piece * (16 / kEs);
-    there = (cols - col) / (16 / kEs);   // (columns are a multiple of 16)
+    there = (cols - col) * kEs;   // (columns are a multiple of 16)
     base = static_cast<const uint8_t*>(p) + (int64_t)first_col * kEs;
     sbase = s;
     off = (uint32_t)row * (uint32_t)pitch + piece * 16;
@@ -68,8 +68,8 @@ struct Stager {
     if (kEight) srsrc = uniform_rsrc(sbase + (int64_t)at * blocks, (uint32_t)rows * (uint32_t)blocks);
   }
   __device__ __forceinline__ void request(int i) {
-    data[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, there > (kEight ? i : 0) ? off : 0x80000000u,
-                                                    kEight ? 16 * i : (uint32_t)(i * (512 / kLanes)) * (uint32_t)pitch, 0);
+    data[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, there > (kEight ? 64 * i : 0) ? off : 0x80000000u,
+                                                    kEight ? 64 * i : (uint32_t)(i * (512 / kLanes)) * (uint32_t)pitch, 0);
   }
   __device__ __forceinline__ void request_scale() {
     if (kEight) byte = __builtin_amdgcn_raw_buffer_load_b8(srsrc, soff, 0, 0);
@@ -83,7 +83,7 @@ struct Stager {
   static constexpr int kParts = kEight ? 2 : 1, kPuts = kN * kParts;
   __device__ __forceinline__ void put(uint16_t* to, int i) const {
     if (kEight) {
-      *reinterpret_cast<bf16x8*>(to + row * kCols + place_of(2 * piece + i, row) * 8) =
+      *reinterpret_cast<bf16x8*>(to + row * kCols + place_of(2 * (piece + 4 * (i / 2)) + i % 2, row) * 8) =
           to_bf16x8(data[i / 2][i % 2 * 2], data[i / 2][i % 2 * 2 + 1], scale_bits(byte));
     } else {
       const int r = row + i * (512 / kLanes);
@@ -136,6 +136,7 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
     if (i < kMB) pf[kk & 1][i] = f;
     else qf[kk & 1][i - kMB] = f;
   };
+  constexpr auto nth_needed = [](int n) { return n == 0 ? kMB : n == 1 ? 0 : n == 2 ? kMB + 1 : n - 2; };   // (read in this order)
   constexpr int kPuts = Stager<kEight, kM>::kPuts + Stager<true, 256>::kPuts;
   auto put = [&](int stage, int i) {
     if (i < qs.kPuts) qs.put(smem + stage * kStage + kRows * kM, i);
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
         __builtin_amdgcn_sched_barrier(0);
         if (kk == 3 && x == 0) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");   // (under the first products)
 #pragma unroll
-        for (int i = x; i < kFrags; i += kMfma) read_frag(kk == 3 ? next : stage, (kk + 1) & 3, i);
+        for (int i = x; i < kFrags; i += kMfma) read_frag(kk == 3 ? next : stage, (kk + 1) & 3, nth_needed(i));
 #pragma unroll
         for (int i = 0; i < kPuts; ++i) {
           if (i * (3 * kMfma) / kPuts == kk * kMfma + x) {   // (spread evenly over the first three quarters)
