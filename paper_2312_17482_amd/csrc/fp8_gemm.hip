@@ -118,12 +118,13 @@ constexpr int kWN = 4, kNB = 2;     // waves along the weight rows, and their bl
 constexpr int kBN = 32 * kWN * kNB, kWaves = 2 * kWN;
 constexpr int kDepth = 2;           // buffers that token fragments rotate through
 
-// Stages of a tile of 64 mb tokens (as many as fit), and LDS in bytes: stages of 64 mb token rows and 256 weight rows, a word for
-// each of 64 scales per wave and stage; the waves' slabs of 32 x 64 bytes for the way out, or the largest magnitudes of a tile's
-// tokens by wave (kAct).
-constexpr int stages_of(int mb) { return mb == 1 ? 3 : 2; }
+// Stages of a tile of 64 mb tokens (as many as fit: 5248 x 4096 x 1024 in tiles of 128 tokens takes 34.6 us with two and 30.8 with
+// three), and LDS in bytes: stages of 64 mb token rows and 256 weight rows, a word for each of 64 scales per wave and stage; the
+// waves' slabs of 32 or 16 tokens x 64 bytes for the way out, or the largest magnitudes of a tile's tokens by wave (kAct).
+constexpr int stages_of(int mb) { return mb <= 2 ? 3 : 2; }
 constexpr int stage_bytes(int mb) { return (64 * mb + kBN) * kStep + kWaves * 256; }
-constexpr int lds_bytes(int mb) { return stages_of(mb) * stage_bytes(mb) + kWaves * 2048; }
+constexpr int slab_rows(int mb) { return mb == 2 ? 16 : 32; }
+constexpr int lds_bytes(int mb) { return stages_of(mb) * stage_bytes(mb) + kWaves * slab_rows(mb) * 64; }
 
 // Workgroup of 8 waves (2 along the tokens by 4 along the weight rows): tiles blockIdx.x, + gridDim.x, ... of 64 kMB tokens
 // x 256 weight rows; a wave computes 32 kMB x 64.
@@ -261,6 +262,8 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
     if (f_tile + (int)gridDim.x < total) {
       f_tile += gridDim.x;
       aim(f_tile);
+    } else {
+      xrsrc[2] = wrsrc[2] = srsrc[2] = 0u;   // (past the last step the loads bring nothing)
     }
   };
 #pragma unroll
@@ -446,10 +449,11 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
         if (wn == 0 && eg == 0 && row < T) pr.out_s[(int64_t)row * (pr.gate_row / kFp8Block) + n0 / kFp8Block] = (uint8_t)byte;
       }
     } else {
-      // 32 tokens x 64 bytes at a time through the wave's own slab, out of which rows leave as 64-byte segments.  (Piece x
+      // 32 tokens (or 16 and 16) x 64 bytes at a time through the wave's own slab, out of which rows leave as 64-byte segments.  (Piece x
       // of a row at position x ^ (row / 4) % 4; the LDS operations of one wave complete in order.)
       constexpr int kEs = kMode == kF32 ? 4 : 2, kCols = 64 / kEs;   // columns of a pass
-      uint8_t* slab = after + wave * 2048;
+      constexpr int kSlab = slab_rows(kMB);
+      uint8_t* const slab = after + wave * (kSlab * 64);
       const int orow = lane >> 2, opiece = lane & 3;
       const __amdgpu_buffer_rsrc_t ors = uniform_rsrc(static_cast<uint8_t*>(pr.out) + (int64_t)m0 * pr.ldo * kEs,
                                                       (uint32_t)min(T - m0, kBM) * (uint32_t)pr.ldo * kEs);
@@ -458,27 +462,32 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
 #pragma unroll
         for (int pass = 0; pass < 32 * kNB / kCols; ++pass) {
           const int nb = pass * kCols / 32, part = pass * kCols % 32;
-          if (kMode == kF32) {
+          auto fill = [&] {
+            uint8_t* const to = slab + (c & (kSlab - 1)) * 64;
+            if (kMode == kF32) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {   // columns 8 j + 4 g .. + 3 of the pass: piece 2 j + g
-              const int v = 4 * (j + part / 8);
-              const float4 w = make_float4(acc[nb][mb][v], acc[nb][mb][v + 1], acc[nb][mb][v + 2], acc[nb][mb][v + 3]);
-              *reinterpret_cast<float4*>(&slab[c * 64 + (((2 * j + g) ^ ((c >> 2) & 3)) * 16)]) = w;
-            }
-          } else {
+              for (int j = 0; j < 2; ++j) {   // columns 8 j + 4 g .. + 3 of the pass: piece 2 j + g
+                const int v = 4 * (j + part / 8);
+                *reinterpret_cast<float4*>(to + (((2 * j + g) ^ ((c >> 2) & 3)) * 16)) =
+                    make_float4(acc[nb][mb][v], acc[nb][mb][v + 1], acc[nb][mb][v + 2], acc[nb][mb][v + 3]);
+              }
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              u32x2 w;
-              w[0] = pack_bf16(acc[nb][mb][4 * j], acc[nb][mb][4 * j + 1]);
-              w[1] = pack_bf16(acc[nb][mb][4 * j + 2], acc[nb][mb][4 * j + 3]);
-              *reinterpret_cast<u32x2*>(&slab[c * 64 + ((j ^ ((c >> 2) & 3)) * 16) + 8 * g]) = w;
+              for (int j = 0; j < 4; ++j) {
+                u32x2 w;
+                w[0] = pack_bf16(acc[nb][mb][4 * j], acc[nb][mb][4 * j + 1]);
+                w[1] = pack_bf16(acc[nb][mb][4 * j + 2], acc[nb][mb][4 * j + 3]);
+                *reinterpret_cast<u32x2*>(to + ((j ^ ((c >> 2) & 3)) * 16) + 8 * g) = w;
+              }
             }
-          }
+          };
           const int col = n0 + wn * kWaveCols + pass * kCols + opiece * (16 / kEs);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
+          for (int u = 0; u < 2; ++u) {   // 16 tokens each
+            if (kSlab == 16 ? c >> 4 == u : u == 0) fill();
+            asm volatile("" : : : "memory");   // (other lanes have written: what a lane that has not sees is new to it, too)
             const int r = 16 * u + orow, t = wm * (32 * kMB) + mb * 32 + r;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(&slab[r * 64 + ((opiece ^ ((r >> 2) & 3)) * 16)]);
+            const u32x4 w = *reinterpret_cast<const u32x4*>(&slab[(r & (kSlab - 1)) * 64 + ((opiece ^ ((r >> 2) & 3)) * 16)]);
             // (what is out of range: an offset past the descriptor, the store is dropped)
             const uint32_t off = ((uint32_t)t * (uint32_t)pr.ldo + (uint32_t)col) * kEs;
             const uint32_t to = m0 + t < T && col < w_rows ? off : 0xffffffe0u;
@@ -722,12 +731,13 @@ void launch_tiles(Product pr, int cols, hipStream_t stream) {
 }
 
 // Estimated microseconds in tiles of 64 `mb` tokens: rounds over the compute units, a step and a tile's start and end each.
-// (Fitted to 20 shapes of 945 to 32768 tokens, which it meets within a fifth, such as, 64 / 128 / 192 / 256 tokens:
-// 945 x 768 x 2304 7.7 / 9.4 / 11.2 / 11.6 us, 8000 x 768 x 2304 24.4 / 24.0 / 21.4 / 23.8, 26963 x 3072 x 768 80 / 75 / 63 / 66,
-// 32768 x 4096 x 4096 - / 615 / 516 / 442; the activation 945 x 768 x 2 x 3072 16.9 / 14.5 / 17.7 / 19.7.)
+// (Fitted to 25 shapes of 945 to 32768 tokens, most of which it meets within a sixth, such as, 64 / 128 / 192 / 256 tokens: 2000 x
+// 768 x 2304 12.4 / 10.5 / 11.7 / 12.3 us, 12000 x 768 x 768 16.4 / 17.0 / 13.0 / 13.2, 5248 x 4096 x 1024 38.9 / 29.6 / 38.0 /
+// 39.0, 8000 x 2048 x 2048 44.7 / 35.5 / 44.3 / 31.7, 32768 x 4096 x 4096 - / 615 / 516 / 432; the activation 945 x 768 x 2 x 3072
+// 15.0 / 12.6 / 14.7 / 16.2, 26963 x 768 x 2 x 3072 223 / 171 / 159 / 141.)
 template <int kMode>
 double tile_cost(int T, int cols, int K, int mb) {
-  constexpr double step[5] = {0, 0.55, 0.92, 1.2, 1.4}, ends[5] = {0, 1.2, 2.0, 2.2, 2.5}, gate[5] = {0, 1.0, 1.4, 3.1, 5.3};
+  constexpr double step[5] = {0, 0.55, 0.85, 1.2, 1.4}, ends[5] = {0, 1.2, 2.0, 2.2, 2.5}, gate[5] = {0, 1.0, 1.4, 1.8, 2.7};
   const int64_t tiles = ((int64_t)T + 64 * mb - 1) / (64 * mb) * ((cols + 255) / 256);
   const double product = step[mb] * (is_exact(kMode) ? 1.6 : 1.0) * fp8_blocks(K) + ends[mb] + (kMode == kAct ? gate[mb] : 0.0);
   return 3.5 + (double)((tiles + kComputeUnits - 1) / kComputeUnits) * product;
