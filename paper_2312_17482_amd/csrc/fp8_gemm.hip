@@ -772,7 +772,7 @@ void launch_product(const Product& pr, int cols, hipStream_t stream) {
   };
   for (int mb = 1; mb <= (is_exact(kMode) ? 3 : 4); ++mb) offer(mb, tile_cost<kMode>(T, cols, K, mb));
   if constexpr (kMode != kAct) {
-    if (T <= 4096) {   // (a grid has 65535 rows of workgroups at most; never the least beyond)
+    if (T <= 4096) {   // (beyond, tiles are the fastest way, or for fp32 results of some 64 columns the second by a sixth)
       offer(11, slice_cost(T, cols, K));
       offer(132, ring_cost(T, cols, K, 1, 1));
       offer(164, ring_cost(T, cols, K, 1, 2));
