@@ -420,6 +420,9 @@ MB_API mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t
  *   hg, hgs     dev, h | g [T_cap, 2*inter]: bf16 with hgs NULL (x (W1 | V) by mb_linear_fp8_fwd), or 8-bit rows.  Read.
  *   dhgq, dhgs  dev, rows [T_cap, 2*inter], written.
  * inter is a multiple of 128 (MB_ERR_UNSUPPORTED otherwise), 2 * inter * hidden < 2^31.
+ * Scales are those of the exact values wherever fp32 sums could decide otherwise: values within 3e-4 of 448 * 2^e that may be a
+ * block's largest are computed again in 64 bits.  That is some hundredths of the time; a batch made of little else (every
+ * column of every token just below a border) takes some hundred times as long.
  */
 MB_API mb_status mb_geglu_fp8_act(const uint8_t* xq, const uint8_t* xs, const uint8_t* w1vq, const uint8_t* w1vs, int T_cap,
                                   const int32_t* meta_dev, int hidden, int inter, uint8_t* actq, uint8_t* acts, void* stream);

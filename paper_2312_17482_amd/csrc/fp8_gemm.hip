@@ -420,6 +420,8 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
         const float value = fabsf(round_beside_border(gated_value64(pr, row, col, l)));
         if (l == who) mine &= mine - 1;
         if ((l & 31) == (who & 31)) {
+          // (one beyond the border decides for the token)
+          if ((__float_as_uint(value) & 0x7fffffu) > 0x600000u) mine &= ~(0xffffull << (which & 48));
 #pragma unroll
           for (int mb = 0; mb < kMB; ++mb)
             if (which >> 4 == mb) top64[mb] = fmaxf(top64[mb], value);

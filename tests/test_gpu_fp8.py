@@ -334,6 +334,21 @@ def test_act_of_equal_rows_on_a_border():
     assert np.all(exps(s) == want) and np.all(np.abs(val(q) * np.ldexp(1.0, want[0, 0]) / 448 - 1) <= 2.0 ** -4)
 
 
+def test_act_one_column_of_many_decides():
+    """All of a token's columns lie just below the border; in half of the blocks a single one, early or late, lies beyond it."""
+    T, hidden, inter = 40, 128, 1024
+    x, w = np.zeros((T, hidden)), np.zeros((2 * inter, hidden))
+    x[:, 0], x[:, 1] = 16.0, 1.0
+    w[:inter, 0], w[:inter, 1] = 1.0, -2.0 ** -13                 # 448 (1 - 2^-17)
+    beyond = [0, 300, 512 + 127, 768 + 64]
+    w[beyond, 1] = 2.0 ** -13                                     # 448 (1 + 2^-17)
+    w[inter:, 0] = 1.75
+    (xv, xq, xs), (wv, wq, ws) = stored(x), stored(w, 128)
+    q, s = mb.mb_geglu_fp8_act(xq, xs, wq, ws)
+    want = orc.scale_exponents(orc.gelu(xv @ wv[:inter].T)[0] * (xv @ wv[inter:].T))
+    assert len(np.unique(want[0])) == 2 and np.all(want == want[0]) and np.array_equal(exps(s), want)
+
+
 @pytest.mark.parametrize("eight", [False, True])
 @pytest.mark.parametrize("T,inter", [(1, 128), (5, 256), (33, 128), (300, 640)])
 def test_gate_backward(T, inter, eight):
