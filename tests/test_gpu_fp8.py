@@ -258,6 +258,76 @@ def test_weight_gradient_of_no_rows_is_zero():
     assert torch.all(dw == 0)
 
 
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("T_cap,T,n_in,n_out", [(700, 333, 768, 528), (4097, 1501, 272, 400), (6000, 65, 784, 2064), (12000, 11999, 528, 528)])
+def test_weight_gradient_reads_nothing_behind_the_last_row(T_cap, T, n_in, n_out, eight):
+    rng = np.random.default_rng(T)
+    _, xq, xs = stored(rows_of(rng, T_cap, n_in))
+    dy = dev(bf16(rows_of(rng, T_cap, n_out)), BF16)
+    dyq, dys = mb.mb_fp8_quant(dy) if eight else (dy, None)
+    meta = torch.tensor([T, 0], dtype=torch.int32, device="cuda")
+    clean = mb.mb_linear_fp8_wgrad(dyq, xq, xs, dys=dys, meta=meta)
+    xq.view(torch.uint8)[T:], xs.view(torch.uint8)[T:] = 0x7f, 255
+    if eight:
+        dyq.view(torch.uint8)[T:], dys.view(torch.uint8)[T:] = 0xff, 255
+    else:
+        dyq[T:] = float("nan")
+    assert torch.equal(mb.mb_linear_fp8_wgrad(dyq, xq, xs, dys=dys, meta=meta), clean) and torch.isfinite(clean).all()
+    for none in (0, -7, -5000):
+        meta[0] = none
+        assert not mb.mb_linear_fp8_wgrad(dyq, xq, xs, dys=dys, meta=meta).any()
+
+
+def test_split_weight_gradient_captured_with_a_workspace_of_its_own():
+    T, n_in, n_out = 12000, 528, 528
+    need = mb.mb_linear_fp8_wgrad_workspace_bytes(T, n_in, n_out)
+    assert need > 0
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    xq, xs = mb.mb_fp8_quant(torch.randn((T, n_in), generator=gen, device="cuda"))
+    dy = torch.randn((T, n_out), generator=gen, device="cuda").to(BF16)
+    work, dw = torch.empty(need, dtype=torch.uint8, device="cuda"), torch.empty((n_out, n_in), device="cuda")
+    mb.mb_linear_fp8_wgrad(dy, xq, xs, dw=dw, workspace=work)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        mb.mb_linear_fp8_wgrad(dy, xq, xs, dw=dw, workspace=work)
+    for _ in range(3):
+        dy.copy_(torch.randn((T, n_out), generator=gen, device="cuda"))
+        work.fill_(0xff)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dw, mb.mb_linear_fp8_wgrad(dy, xq, xs))
+
+
+def test_row_counts_of_nothing():
+    """A count of zero, or a negative one, on the device: nothing is written, by any way through the products."""
+    rng = np.random.default_rng(4)
+    meta = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for T_cap, n_in, n_out in ((33, 272, 144), (300, 784, 784), (500, 3088, 784), (700, 528, 784), (2500, 784, 784), (4100, 144, 1040),
+                               (6200, 144, 3088), (12000, 144, 2064)):
+        _, xq, xs = stored(rows_of(rng, T_cap, n_in))
+        wq, ws = mb.mb_fp8_quant_weight(torch.ones((n_out, n_in), device="cuda"), transposed=False)
+        for none in (0, -1, -7000):
+            meta[0] = none
+            for dtype in (BF16, F32):
+                y = torch.full((T_cap, n_out), 5.0, dtype=dtype, device="cuda")
+                assert torch.all(mb.mb_linear_fp8_fwd(xq, xs, wq, ws, meta=meta, y=y) == 5.0)
+    for T_cap, hidden, inter in ((200, 144, 256), (3000, 144, 1152), (4100, 144, 2176), (8190, 400, 1024)):
+        _, xq, xs = stored(rows_of(rng, T_cap, hidden))
+        wq, ws = mb.mb_fp8_quant_weight(torch.ones((2 * inter, hidden), device="cuda"), transposed=False)
+        da, hg = torch.ones((T_cap, inter), dtype=BF16, device="cuda"), torch.ones((T_cap, 2 * inter), dtype=BF16, device="cuda")
+        for none in (0, -1, -7000):
+            meta[0] = none
+            q, s = torch.full((T_cap, inter), 7, dtype=torch.uint8, device="cuda"), torch.full((T_cap, inter // 128), 9, dtype=torch.uint8, device="cuda")
+            mb.mb_geglu_fp8_act(xq, xs, wq, ws, meta=meta, actq=q.view(E4M3), acts=s.view(E8M0))
+            assert torch.all(q == 7) and torch.all(s == 9)
+            mb.mb_fp8_quant(da, meta=meta, q=q.view(E4M3), s=s.view(E8M0))
+            assert torch.all(q == 7) and torch.all(s == 9)
+            dq, ds = torch.full((T_cap, 2 * inter), 7, dtype=torch.uint8, device="cuda"), torch.full((T_cap, inter // 64), 9, dtype=torch.uint8, device="cuda")
+            mb.mb_gelu_gate_fp8_bwd(da, hg, meta=meta, dhgq=dq.view(E4M3), dhgs=ds.view(E8M0))
+            assert torch.all(dq == 7) and torch.all(ds == 9)
+
+
 # ---------------------------------------------------------------------------------------------------- the gate
 def check_eight(q, s, v, err):
     """8-bit rows against values v known within err."""
