@@ -25,7 +25,6 @@ constexpr int kF32 = 1;    // out = product in fp32
 constexpr int kAct = 2;    // out = GeLU(x W1) (*) x V in 8 bits, and its scales (weight = W1^T over V^T)
 
 constexpr int kStep = 128;    // k per stage, bytes per staged row
-constexpr int kGroupM = 4;    // token panels walked together (L2 reuse of the weight tiles)
 
 constexpr bool is_exact(int mode) { return mode == kF32; }
 
@@ -154,15 +153,19 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
   constexpr int kOutCols = kGated ? kBN / 2 : kBN;
   const int nk = blocks;
 
-  // Tile id -> token panel, weight tile: every XCD a contiguous run of tiles, kGroupM token panels at a time.
+  // Tile id -> token panel, weight tile: every XCD a contiguous run of tiles, 4 token panels at a time (of 256 tiles an XCD has
+  // 32: 4 by 8), or 12 where a workgroup has several tiles.  (4 and 12 panels: 4000 x 1024 x 4096, one tile each, 20.5 and 22.0 us;
+  // several: 26963 x 768 x 2304 68 and 61, 16384 x 1024 x 4096 77 and 74, 20000 x 2048 x 2048 87 and 84, 32768 x 4096 x 4096 458 and
+  // 437; of 13 shapes two are slower, 12000 x 4096 x 4096 168 and 173, 32768 x 1024 x 1024 39.5 and 40.9.)
+  const int group_m = kMB == 4 && total > (int)gridDim.x ? 12 : 4;
   auto locate = [&](int id, int& m0, int& n0) {
     const int per = total >> 3;
     int lin = id;
     if (lin < (per << 3)) lin = (lin & 7) * per + (lin >> 3);
-    const int group = lin / (kGroupM * n_tiles);
-    const int first_m = group * kGroupM;
-    const int gsize = min(m_tiles - first_m, kGroupM);
-    const int rem = lin - group * (kGroupM * n_tiles);
+    const int group = lin / (group_m * n_tiles);
+    const int first_m = group * group_m;
+    const int gsize = min(m_tiles - first_m, group_m);
+    const int rem = lin - group * (group_m * n_tiles);
     m0 = __builtin_amdgcn_readfirstlane(first_m + rem % gsize) * kBM;
     n0 = __builtin_amdgcn_readfirstlane(rem / gsize) * kOutCols;
   };
