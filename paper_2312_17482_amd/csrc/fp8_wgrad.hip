@@ -6,7 +6,7 @@
 // bits of significand and a power of two) and multiplied by v_mfma_f32_32x32x16_bf16.  They pass through registers for it: 16 bytes of
 // a row per load, one scale byte each, two 16-byte LDS writes.  The rest is the bf16 weight gradient's way: rows as they are
 // in LDS, operands by transposing reads, 64 kMB x 256 tiles by 8 waves, steps of 64 tokens in two stages, the tokens split over
-// workgroups where the tiles are few, partial tiles added in a fixed order.  26963 x 768 x 6144 takes 234 us, 22 of them the adding;
+// workgroups where the tiles are few, partial tiles added in a fixed order.  26963 x 768 x 6144 takes 232 us, 22 of them the adding;
 // without a step's loads and LDS writes it would take 195, without the conversions 230.
 #include "fp8_util.h"
 
