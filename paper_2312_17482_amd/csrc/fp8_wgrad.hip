@@ -6,8 +6,8 @@
 // bits of significand and a power of two) and multiplied by v_mfma_f32_32x32x16_bf16.  They pass through registers for it: 16 bytes of
 // a row per load, one scale byte each, two 16-byte LDS writes.  The rest is the bf16 weight gradient's way: rows as they are
 // in LDS, operands by transposing reads, 64 kMB x 256 tiles by 8 waves, steps of 64 tokens in two stages, the tokens split over
-// workgroups where the tiles are few, partial tiles added in a fixed order.  26963 x 768 x 6144 takes 232 us, 22 of them the adding;
-// without a step's loads and LDS writes it would take 195, without the conversions 230.
+// workgroups where the tiles are few, partial tiles added in a fixed order.  26963 x 768 x 6144 takes 225 us in three splits, 12 of them
+// the adding.  (Where it took 235, in seven, it took 195 without the steps' loads and LDS writes and 231 without conversions.)
 #include "fp8_util.h"
 
 namespace mb {
@@ -370,7 +370,8 @@ __global__ __launch_bounds__(256) void fp8_wgrad_add_kernel(const float* __restr
 // Splits of the tokens and the tile's height (0: slices) with the least estimated time.  (Fitted to 16 shapes, which it meets
 // within a fifth.  One piece in slices, tiles of 256 and 128 rows: 64 x 768 x 768 4.9 / 8.5 / 6.3 us, 945 x 768 x 768 8.2 / 26 / 18,
 // 945 x 768 x 2304 13.9 / 27 / 18.7, 945 x 768 x 6144 28 / 29 / 21, 2500 x 768 x 768 14.9 / 57 / 39 (in 5 splits 26 / 20.7), 26963 x
-// 768 x 768 94 / 530 / 359 (24 and 14 splits 47 / 44), 26963 x 768 x 6144 638 / 541 / 380 (3 and 5 splits 226 / 277).)
+// 768 x 768 94 / 530 / 359 (24 and 14 splits 47 / 44), 26963 x 768 x 6144 638 / 541 / 380 (3 and 5 splits 226 / 277;
+// in 7 of 256 rows 230).)
 struct Choice {
   int splits, height;
 };
@@ -384,7 +385,8 @@ Choice choose(int T_cap, int n_in, int n_out) {
     const int64_t tiles = (int64_t)((n_out + 64 * mb - 1) / (64 * mb)) * ((n_in + 255) / 256);
     for (int s = 1; s <= kMaxSplits && s <= (steps > 0 ? steps : 1); ++s) {
       const double full = tiles * s < kComputeUnits ? (double)(tiles * s) / kComputeUnits : 1.0;
-      const double step = mb == 4 ? 1.25 + 0.35 * full : 0.85 + 0.2 * full;
+      const double power = full * full * full;   // (a step takes longer as the card fills up and its clock falls)
+      const double step = mb == 4 ? 1.25 + 0.35 * power : 0.85 + 0.2 * power;
       const double cost = 3.0 + (double)((tiles * s + kComputeUnits - 1) / kComputeUnits) * (step * ((steps + s - 1) / s) + 2.5) +
                           (s > 1 ? 2.5 + (s + 1) * bytes / 7e6 : 0.0);
       if (cost < least) {
