@@ -379,6 +379,8 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
                                            // deviation), gelu_tail at most 4.5e-5
       auto all_written = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory"); };
       float* const tops = reinterpret_cast<float*>(after);   // [wn][token of the tile]
+      float* const tops64 = tops + kWN * kBM;                // the same after a second look
+      static_assert(2 * kWN * kBM * sizeof(float) <= kWaves * slab_rows(kMB) * 64, "both take the slabs' place");
       uint8_t* const out = static_cast<uint8_t*>(pr.out);
       const __amdgpu_buffer_rsrc_t ors = uniform_rsrc(out + (int64_t)m0 * pr.ldo, (uint32_t)min(T - m0, kBM) * (uint32_t)pr.ldo);
 #pragma unroll
@@ -389,20 +391,23 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
         if (g == 0) tops[wn * kBM + wm * 32 * kMB + mb * 32 + c] = top;
       }
       all_written();
-      auto top_of = [&](int t) {
-        float a = tops[t];
+      auto most_of = [&](const float* from, int t) {
+        float a = from[t];
 #pragma unroll
-        for (int i = 1; i < kWN; ++i) a = fmaxf(a, tops[i * kBM + t]);
+        for (int i = 1; i < kWN; ++i) a = fmaxf(a, from[i * kBM + t]);
         return a;
       };
+      auto top_of = [&](int t) { return most_of(tops, t); };
       // Tokens whose scale the products' grouping could decide (2 in a tile, and the four waves of a token agree): the values
       // that do so again in 64 bits, one after the other, each by the wave that holds it.
       uint64_t mine = 0;
+      bool again = false;   // the same in all lanes, and in the four waves
 #pragma unroll
       for (int mb = 0; mb < kMB; ++mb) {
         const float top = top_of(wm * 32 * kMB + mb * 32 + c);
         const float from = near_border(top, kReach) ? border_from(top, kReach) : __builtin_inff();
         if (__ballot(near_border(top, kReach))) {
+          again = true;
           uint32_t bits = 0;
 #pragma unroll
           for (int v = 0; v < 16; ++v) bits |= finite_abs(acc[0][mb][v]) >= from ? 1u << v : 0u;
@@ -412,7 +417,6 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
       float top64[kMB];
 #pragma unroll
       for (int mb = 0; mb < kMB; ++mb) top64[mb] = -1.f;
-      const bool again = __ballot(mine != 0) != 0;
       for (uint64_t left; (left = __ballot(mine != 0)) != 0;) {
         const int who = __ffsll((unsigned long long)left) - 1;
         const int which = __builtin_amdgcn_readlane(__ffsll((unsigned long long)mine) - 1, who);
@@ -430,17 +434,20 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
             if (which >> 4 == mb) top64[mb] = fmaxf(top64[mb], value);
         }
       }
+      // (to a place of their own: other waves may still be reading `tops` for what stands above)
       if (again) {
 #pragma unroll
-        for (int mb = 0; mb < kMB; ++mb)
-          if (g == 0 && top64[mb] >= 0.f) tops[wn * kBM + wm * 32 * kMB + mb * 32 + c] = top64[mb];
+        for (int mb = 0; mb < kMB; ++mb) {
+          const int l = lane_again(), t = wm * 32 * kMB + mb * 32 + (l & 31);
+          if (l < 32) tops64[wn * kBM + t] = top64[mb] >= 0.f ? top64[mb] : tops[wn * kBM + t];
+        }
       }
       all_written();
       const int e_lane = lane_again(), ec = e_lane & 31, eg = e_lane >> 5;
 #pragma unroll
       for (int mb = 0; mb < kMB; ++mb) {
         const int t = wm * 32 * kMB + mb * 32 + ec, row = m0 + t;
-        const int byte = scale_byte(top_of(t));
+        const int byte = scale_byte(most_of(again ? tops64 : tops, t));
         uint32_t d[4];   // columns 8 j + 4 g .. + 3
 #pragma unroll
         for (int j = 0; j < 4; ++j)
