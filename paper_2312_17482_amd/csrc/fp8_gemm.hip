@@ -401,22 +401,19 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
       // Tokens whose scale the products' grouping could decide (2 in a tile, and the four waves of a token agree): the values
       // that do so again in 64 bits, one after the other, each by the wave that holds it.
       uint64_t mine = 0;
-      bool again = false;   // the same in all lanes, and in the four waves
+      uint32_t again = 0;   // blocks of 32 tokens with such ones: the same in all lanes, and in the four waves
 #pragma unroll
       for (int mb = 0; mb < kMB; ++mb) {
         const float top = top_of(wm * 32 * kMB + mb * 32 + c);
         const float from = near_border(top, kReach) ? border_from(top, kReach) : __builtin_inff();
         if (__ballot(near_border(top, kReach))) {
-          again = true;
+          again |= 1u << mb;
           uint32_t bits = 0;
 #pragma unroll
           for (int v = 0; v < 16; ++v) bits |= finite_abs(acc[0][mb][v]) >= from ? 1u << v : 0u;
           mine |= (uint64_t)bits << (16 * mb);
         }
       }
-      float top64[kMB];
-#pragma unroll
-      for (int mb = 0; mb < kMB; ++mb) top64[mb] = -1.f;
       for (uint64_t left; (left = __ballot(mine != 0)) != 0;) {
         const int who = __ffsll((unsigned long long)left) - 1;
         const int which = __builtin_amdgcn_readlane(__ffsll((unsigned long long)mine) - 1, who);
@@ -424,30 +421,34 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
         const int row = m0 + wm * 32 * kMB + (which >> 4) * 32 + (who & 31);
         const int col = n0 + wn * 32 + 8 * ((which & 15) >> 2) + 4 * (who >> 5) + (which & 3);
         const int l = lane_again();
-        const float value = fabsf(round_beside_border(gated_value64(pr, row, col, l)));
-        if (l == who) mine &= mine - 1;
-        if ((l & 31) == (who & 31)) {
-          // (one beyond the border decides for the token)
-          if ((__float_as_uint(value) & 0x7fffffu) > 0x600000u) mine &= ~(0xffffull << (which & 48));
-#pragma unroll
-          for (int mb = 0; mb < kMB; ++mb)
-            if (which >> 4 == mb) top64[mb] = fmaxf(top64[mb], value);
-        }
-      }
-      // (to a place of their own: other waves may still be reading `tops` for what stands above)
-      if (again) {
+        const float value = round_beside_border(gated_value64(pr, row, col, l));
+        // It takes the place of the one out of the matrix cores, which may be far from it (sums that cancel): what is stored
+        // is what the scale is taken from.
 #pragma unroll
         for (int mb = 0; mb < kMB; ++mb) {
-          const int l = lane_again(), t = wm * 32 * kMB + mb * 32 + (l & 31);
-          if (l < 32) tops64[wn * kBM + t] = top64[mb] >= 0.f ? top64[mb] : tops[wn * kBM + t];
+          if (which >> 4 != mb) continue;
+#pragma unroll
+          for (int v = 0; v < 16; ++v)
+            if ((which & 15) == v) acc[0][mb][v] = l == who ? value : acc[0][mb][v];
         }
+        if (l == who) mine &= mine - 1;
+        // (one beyond the border decides for the token)
+        if ((l & 31) == (who & 31) && (__float_as_uint(value) & 0x7fffffu) > 0x600000u) mine &= ~(0xffffull << (which & 48));
+      }
+      // (to a place of their own: other waves may still be reading `tops` for what stands above)
+#pragma unroll
+      for (int mb = 0; mb < kMB; ++mb) {
+        if (!(again >> mb & 1)) continue;
+        const float top = max_both_halves(largest_of_16(acc[0][mb]));
+        const int l = lane_again();
+        if (l < 32) tops64[wn * kBM + wm * 32 * kMB + mb * 32 + l] = top;
       }
       all_written();
       const int e_lane = lane_again(), ec = e_lane & 31, eg = e_lane >> 5;
 #pragma unroll
       for (int mb = 0; mb < kMB; ++mb) {
         const int t = wm * 32 * kMB + mb * 32 + ec, row = m0 + t;
-        const int byte = scale_byte(most_of(again ? tops64 : tops, t));
+        const int byte = scale_byte(most_of(again >> mb & 1 ? tops64 : tops, t));
         uint32_t d[4];   // columns 8 j + 4 g .. + 3
 #pragma unroll
         for (int j = 0; j < 4; ++j)

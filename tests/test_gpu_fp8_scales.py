@@ -47,3 +47,30 @@ def test_act_of_cancelling_sums_is_the_same_each_time():
     for _ in range(20):
         _, _, _, q2, s2 = act(x, w)
         assert torch.equal(q.view(torch.uint8), q2.view(torch.uint8)) and torch.equal(s.view(torch.uint8), s2.view(torch.uint8))
+
+
+def test_act_of_cancelling_sums_stays_finite():
+    """Where 64 bits move a value far from what the matrix cores made of it, and the scale with it, what is stored fits that scale:
+    the value lies between the exact one and three times it, never beyond e4m3."""
+    x, w = cancelling()
+    v, q, e, _, _ = act(x, w)
+    got = q * np.repeat(np.ldexp(1.0, e), 128, 1)
+    assert np.isfinite(q).all()
+    ratio = got / v                                               # (GeLU(-3 a) / GeLU(-a) < 3; a rounding is 2^-4)
+    assert np.all((ratio >= 1 - 2.0 ** -4) & (ratio <= 3 * (1 + 2.0 ** -4)))
+    # a block that was looked at again holds the exact values
+    again = np.all(np.abs(ratio - 1) <= 2.0 ** -4, 1)
+    print(again.sum(), "tokens looked at again")
+    assert again.any() and np.array_equal(e[again], orc.scale_exponents(v)[again])
+
+
+def test_act_value_beside_a_cancelling_one():
+    """One column is computed at the border and is a third of it; the others, just under what is looked at again, need the scale."""
+    x, w = cancelling()
+    w[1:128], w[129:] = 0.0, 0.0
+    w[128] *= -256.0                                              # computed as 333 .. 666
+    x[:, 16], x[:, 24] = 16.0, 1.0
+    w[1:32, 16], w[129:160, 24] = 1.0, 26.0                       # 416, whose scale is 448's
+    v, q, e, _, _ = act(x, w)
+    got = q * np.repeat(np.ldexp(1.0, e), 128, 1)
+    assert np.all(np.abs(got[:, 1:32] / 416 - 1) <= 2.0 ** -4)
