@@ -432,8 +432,9 @@ __device__ __forceinline__ void fp8_tiles(const Product& pr, int T, uint8_t* __r
             if ((which & 15) == v) acc[0][mb][v] = l == who ? value : acc[0][mb][v];
         }
         if (l == who) mine &= mine - 1;
-        // (one beyond the border decides for the token)
-        if ((l & 31) == (who & 31) && (__float_as_uint(value) & 0x7fffffu) > 0x600000u) mine &= ~(0xffffull << (which & 48));
+        // (one beyond the border decides for the token; the border is that of the computed values: this one may be far from it)
+        const float border = border_from(top_of(wm * 32 * kMB + (which >> 4) * 32 + (who & 31)), 0);
+        if ((l & 31) == (who & 31) && fabsf(value) > border) mine &= ~(0xffffull << (which & 48));
       }
       // (to a place of their own: other waves may still be reading `tops` for what stands above)
 #pragma unroll

@@ -74,3 +74,17 @@ def test_act_value_beside_a_cancelling_one():
     v, q, e, _, _ = act(x, w)
     got = q * np.repeat(np.ldexp(1.0, e), 128, 1)
     assert np.all(np.abs(got[:, 1:32] / 416 - 1) <= 2.0 ** -4)
+
+
+def test_act_a_value_far_below_the_border_does_not_end_the_search():
+    """Column 0 of a token is computed beside 448 and is 0.503 of it, a mantissa over 1.75; column 5 is 448 (1 + 2^-17) and computed as
+    448: it decides, however early the other one is looked at."""
+    x, w = octave(), np.zeros((256, 128))
+    x[:, 0], x[:, 1], x[:, 2], x[:, 8] = 448.0, 448.0, 1.0, 1.0
+    w[0, 0], w[0, 1], w[0, 2], w[0, 8] = 1.0, -1.0, 0.0390625, -0.046875
+    w[128, [64, 72, 80]] = -192.0
+    x[:, 16], x[:, 17], x[:, 24] = 16.0, 1.0, 16.0
+    w[5, 16], w[5, 17] = 1.0, 2.0 ** -13
+    w[128 + 5, 24] = 1.75
+    v, q, e, _, _ = act(x, w)
+    assert np.array_equal(orc.scale_exponents(v), np.ones((len(x), 1))) and np.all(e == 1)
