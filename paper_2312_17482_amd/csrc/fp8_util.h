@@ -99,21 +99,10 @@ __device__ __forceinline__ float max_of_8_lanes(float x) {
   return fmaxf(x, __shfl_xor(x, 4));
 }
 
-// Phi(-|h|) and exp(-h^2 / 2) for the GeLU, Phi the normal distribution function.  With x = |h| / sqrt 2:
-//   Phi(-|h|) = erfc(x) / 2 = t P(t) exp(-x^2) / 2,  t = 1 / (1 + 0.53 x),
-// P of degree 4 through erfc(x) exp(x^2) / t, fitted for the least RELATIVE error over x = 0 .. 9.5 (2.9e-5).  Relative, because a
-// block whose gates are all far negative gets a scale of its own: there an absolute error of 1e-7, enough for a bf16 result next
-// to larger ones, would be most of the value.  A stored result is rounded by 2^-4 of itself; where 2.9e-5 could decide the
-// block's scale, 64 bits do.
-__device__ __forceinline__ float normal_tail(float h, float& e) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(0.53f * 0.70710678118654752f, fabsf(h), 1.0f));
-  float p = fmaf(0.5f * -0.1819639537601447f, t, 0.5f * 0.4030186555514750f);
-  p = fmaf(p, t, 0.5f * 0.1652416641586280f);
-  p = fmaf(p, t, 0.5f * 0.3158106802747941f);
-  p = fmaf(p, t, 0.5f * 0.2978819081133195f);
-  e = __builtin_amdgcn_exp2f(h * (h * (-0.5f * kLog2e)));
-  return p * t * e;
-}
+// The GeLU with a small RELATIVE error, because a block whose gates are all far negative gets a scale of its own: there an absolute
+// error of 1e-7, enough for a bf16 result next to larger ones, would be most of the value.  A stored result is rounded by 2^-4 of
+// itself; where the error could decide the block's scale, 64 bits do.  (Phi the normal distribution function, phi its density.)
+//
 // GeLU(h) = h Phi(h) = max(h, 0) - |h| Phi(-|h|) alone, where the derivative's exp(-h^2 / 2) is not needed as well: Phi(-|h|) as
 // 2^Q(|h|), Q of degree 9 fitted for the least error over |h| = 0 .. 13.4, 2.4e-5 of the value (with fp32's rounding 3.4e-5 up to
 // 11 and 4.5e-5 beyond).  One transcendental instead of two, which take as long as four other instructions each.  (Q falls
@@ -132,13 +121,27 @@ __device__ __forceinline__ float gelu_tail(float h) {
   const float above = __uint_as_float((uint32_t)max((int)__float_as_uint(h), 0));   // max(h, 0), without quieting a NaN first
   return fmaf(-x, __builtin_amdgcn_exp2f(q), above);
 }
-// The same and the derivative Phi(h) + h phi(h).
+// The same and the derivative Phi(h) + h phi(h), which are a rational form times exp(-h^2 / 2) each.  With x = |h|, t = 1 / (1 + 0.3748 x):
+//   Phi(-x)            = t P(t) exp(-x^2 / 2),
+//   Phi(-x) - x phi(x) = (x0 - x) S(t) exp(-x^2 / 2),  x0 = 0.75179152 the zero of the derivative,
+// P and S of degree 4 fitted for the least relative error over x = 0 .. 13.4.  The zero stands as a factor of its own: as the difference
+// of the two terms, 3e-5 of either were 0.8 % of the derivative at -0.75.  (Of all bf16 h down to -13, which hold all that a stored
+// h can be: 3.2e-5 of the value and 3.0e-5 of the derivative, 1e-5 within 0.1 of its zero; x0 - x is exact there and x0's own
+// rounding 7e-6 of the least of it.)
 __device__ __forceinline__ void gelu_tail_and_grad(float h, float& val, float& grad) {
-  float e;
-  const float u = normal_tail(h, e);
-  val = fmaf(-fabsf(h), u, fmaxf(h, 0.0f));
-  const float cdf = h < 0.f ? u : 1.0f - u;
-  grad = fmaf(h * 0.3989422804014327f, e, cdf);
+  const float x = fabsf(h), t = __builtin_amdgcn_rcpf(fmaf(0.3748f, x, 1.0f));
+  float p = fmaf(-0.0910138860f, t, 0.201512620f);
+  p = fmaf(p, t, 0.0826170594f);
+  p = fmaf(p, t, 0.157924652f);
+  p = fmaf(p, t, 0.148953438f);
+  float s = fmaf(-0.0353672020f, t, 0.129396364f);
+  s = fmaf(s, t, 0.0526783615f);
+  s = fmaf(s, t, 0.120035514f);
+  s = fmaf(s, t, 0.398352832f);
+  const float e = __builtin_amdgcn_exp2f(h * (h * (-0.5f * kLog2e)));
+  val = fmaf(-x, p * t * e, fmaxf(h, 0.0f));
+  const float below = s * (0.75179154f - x) * e;   // the derivative at -x; at x it is 1 - that
+  grad = h < 0.f ? below : 1.0f - below;
 }
 // Largest finite magnitude of 16 values.
 template <typename V>
@@ -179,7 +182,8 @@ __device__ __forceinline__ double wave_sum(double x) {
   return joined(c[0], d[0]) + joined(c[1], d[1]);
 }
 
-// GeLU in 64 bits, and its derivative: normal_tail's form with t = 1 / (1 + 0.3 x) and P of degree 10 (4e-10 of the value), to decide between scales.
+// GeLU in 64 bits, and its derivative: Phi(-|h|) = t P(t) exp(-x^2) / 2 with x = |h| / sqrt 2, t = 1 / (1 + 0.3 x) and P of degree 10 (4e-10
+// of the value, and of Phi in the derivative), to decide between scales.
 __device__ __forceinline__ double gelu64(double h, double* grad = nullptr) {
   const double x = fabs(h) * 0.70710678118654752440, t = 1.0 / fma(0.3, x, 1.0);
   double p = 0.055734015794935123;
