@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
   for (int i = 0; i < 16; ++i) {
     float val, grad;
     gelu_tail_and_grad(h[i], val, grad);
-    h[i] = a[i] * g[i] * grad;
+    h[i] = a[i] * (g[i] * grad);   // (a g may be beyond the largest float where the derivative is next to nothing)
     g[i] = a[i] * val;
     if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (four values at a time: with all 16 interleaved 115 us instead of 104)
   }

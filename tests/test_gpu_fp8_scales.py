@@ -137,3 +137,16 @@ def test_gate_backward_scales_are_the_definitions(eight):
     clear = np.abs(top / beside - 1) > 1e-8
     assert clear.sum() > 191980 and (np.abs(top / beside - 1) < 7e-5).sum() >= (1 if eight else 4)   # (values of few bits)
     assert np.array_equal(exps(s)[clear], orc.scale_exponents(v)[clear])
+
+
+def test_gate_backward_of_large_factors_with_a_small_slope():
+    """da g beyond the largest float times a slope that is next to nothing is a finite value, or zero."""
+    da, hg = np.zeros((3, 128)), np.zeros((3, 256))
+    da[:, 0], hg[:, 128] = 2.0 ** 70, 2.0 ** 70
+    hg[:, 0] = [-30.0, -9.0, -12.0]
+    q, s = mb.mb_gelu_gate_fp8_bwd(dev(da, BF16), dev(hg, BF16))
+    value, slope = orc.gelu(hg[:, :1])
+    want = (da[:, :1] * hg[:, 128:129] * slope)[:, 0]
+    got = val(q)[:, 0] * np.ldexp(1.0, exps(s)[:, 0])
+    assert np.isfinite(val(q)[:, :128]).all() and got[0] == 0.0
+    assert np.all(np.abs(got - want)[1:] <= 2.0 ** -4 * (1 + 1e-3) * np.abs(want)[1:])
