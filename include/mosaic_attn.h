@@ -420,9 +420,13 @@ MB_API mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t
  *   hg, hgs     dev, h | g [T_cap, 2*inter]: bf16 with hgs NULL (x (W1 | V) by mb_linear_fp8_fwd), or 8-bit rows.  Read.
  *   dhgq, dhgs  dev, rows [T_cap, 2*inter], written.
  * inter is a multiple of 128 (MB_ERR_UNSUPPORTED otherwise), 2 * inter * hidden < 2^31.
- * Scales are those of the exact values wherever fp32 sums could decide otherwise: values within 3e-4 of 448 * 2^e that may be a
- * block's largest are computed again in 64 bits.  That is some hundredths of the time; a batch made of little else (every
- * column of every token just below a border) takes some hundred times as long.
+ * Scales: a block's scale is taken from the values that are stored, so that it holds every finite one.  Where the largest lies within
+ * 2.8e-4 (mb_geglu_fp8_act) or 7e-5 (mb_gelu_gate_fp8_bwd) of 448 * 2^e, the values that decide are computed again in 64 bits (and
+ * stored as such by mb_geglu_fp8_act).  Scales are therefore those of the exact values wherever the computed ones are that near to
+ * them.  The gate's backward is, 3.3e-5 at most; the activation is, with 1.4e-5 to 4.4e-5, unless its sums cancel or one product
+ * of a group is far larger than the result: then a scale can be a neighbour of the exact values', as the value itself is off.
+ * Time: some hundredths; a batch made of little else (every column of every token just below a border) takes some hundred times
+ * as long.
  */
 MB_API mb_status mb_geglu_fp8_act(const uint8_t* xq, const uint8_t* xs, const uint8_t* w1vq, const uint8_t* w1vs, int T_cap,
                                   const int32_t* meta_dev, int hidden, int inter, uint8_t* actq, uint8_t* acts, void* stream);

@@ -5,7 +5,7 @@ import torch
 
 from oracle import fp8_oracle as orc
 from paper_2312_17482_amd import binding as mb
-from tests.test_gpu_fp8 import BF16, bf16, dev, exps, stored, val
+from tests.test_gpu_fp8 import BF16, bf16, check_eight, dev, exps, stored, val
 
 pytestmark = pytest.mark.gpu
 
@@ -150,3 +150,40 @@ def test_gate_backward_of_large_factors_with_a_small_slope():
     got = val(q)[:, 0] * np.ldexp(1.0, exps(s)[:, 0])
     assert np.isfinite(val(q)[:, :128]).all() and got[0] == 0.0
     assert np.all(np.abs(got - want)[1:] <= 2.0 ** -4 * (1 + 1e-3) * np.abs(want)[1:])
+
+
+@pytest.mark.parametrize("mean,xs,ws,low,high", [(5.8, 0.1, 0.3, -6.5, -5.0), (8.5, 0.5, 2.0, -13.0, -5.0)])
+def test_act_scales_of_far_negative_gates(mean, xs, ws, low, high):
+    """Every gate of 24,000 blocks far below zero, sums of 768 products: an error of h is h^2 times as much of GeLU(h)."""
+    T, hidden, inter = 12000, 768, 256
+    rng = np.random.default_rng(77)
+    x, xq, xsc = stored(1.0 + xs * rng.standard_normal((T, hidden)))
+    w = np.concatenate([-(mean / hidden) * (1.0 + ws * rng.standard_normal((inter, hidden))), 0.03 * rng.standard_normal((inter, hidden))])
+    w, wq, wsc = stored(w, 128)
+    hg = x @ w.T
+    h = hg[:, :inter]
+    assert h.max() < high and h.min() > low
+    v = orc.gelu(h)[0] * hg[:, inter:]
+    top = np.abs(v).reshape(T, 2, 128).max(2)
+    beside = np.ldexp(448.0, np.floor(np.log2(top / 448.0) + 0.5).astype(int))
+    clear = np.abs(top / beside - 1) > 1e-8                       # (GeLU in 64 bits is good to 4e-10)
+    _, s = mb.mb_geglu_fp8_act(xq, xsc, wq, wsc)
+    wrong = exps(s) != orc.scale_exponents(v)
+    print(wrong.sum(), "of", wrong.size, "scales;", (np.abs(top / beside - 1) < 1e-3).sum(), "blocks within 1e-3 of a border")
+    assert not wrong[clear].any()
+
+
+def test_act_beside_one_large_channel():
+    """One channel moves every gate to -9: its product outweighs those it is added with, of which it keeps 2^-10.  Values and scales
+    are within what that leaves, 7 * 2^-13 of the sums of magnitudes."""
+    T, hidden, inter = 3000, 768, 256
+    rng = np.random.default_rng(79)
+    x, w = rng.standard_normal((T, hidden)), 0.03 * rng.standard_normal((2 * inter, hidden))
+    x[:, 5], w[:inter, 5], w[inter:, 5] = 12.0, -0.75, 0.0
+    (x, xq, xs), (w, wq, ws) = stored(x), stored(w, 128)
+    q, s = mb.mb_geglu_fp8_act(xq, xs, wq, ws)
+    hg, eps = x @ w.T, (7 * 2.0 ** -13 + (hidden + 8) * 2.0 ** -24) * (np.abs(x) @ np.abs(w).T)
+    h, g = hg[:, :inter], hg[:, inter:]
+    value, off = orc.gelu(h)[0], np.abs(orc.gelu(h + eps[:, :inter])[0] - orc.gelu(h)[0])
+    assert h.max() < -4 and np.isfinite(val(q)).all()
+    check_eight(q, s, value * g, off * (np.abs(g) + eps[:, inter:]) + np.abs(value) * eps[:, inter:] + 5e-5 * np.abs(value * g))
