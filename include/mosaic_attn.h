@@ -382,9 +382,16 @@ MB_API mb_status mb_fp8_quant_weight(const void* w, int n_out, int n_in, mb_dtyp
                                      uint8_t* st, void* stream);
 
 /*
- * Linear layer on 8-bit rows:  y[t, n] = sum_k x[t, k] w[n, k], fp32 sums, rounded once to dt.
+ * Linear layer on 8-bit rows:  y[t, n] = sum_k x[t, k] w[n, k].
  *   xq, xs   dev, rows [T_cap, n_in], read.      wq, ws   dev, weight [n_out, n_in], read.
  *   y        dev, [T_cap, n_out] of row stride y_row_stride, written.
+ *   dt       the result's type, and how its sums are taken:
+ *     MB_F32   fp32 sums of products of bf16 operands, which hold 8-bit values exactly from 2^-126 up to 2^128.
+ *     MB_BF16  the 8-bit matrix instructions, twice as fast, whose sums are less than fp32 ones: products of 8 neighbouring k are
+ *              aligned to the largest of them and keep 13 bits below its leading one, these partial sums are added in fp32; rounded
+ *              once to bf16.  Beside that rounding the error is at most 7 * 2^-13 of sum_k |x w|: 1.5e-5 of a result's own size
+ *              for operands of random signs, more where a sum cancels.  A caller who needs fp32 sums asks for MB_F32.
+ * Sums are taken in a fixed order that depends on the sizes (T_cap among them) only.
  * The data gradient dx = dy W is the same call: rows dy [T_cap, n_out] with the transposed weight qt, st of mb_fp8_quant_weight.
  * T_cap * n_out < 2^38.
  */
@@ -411,7 +418,8 @@ MB_API mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t
  * The GeGLU feed-forward on 8-bit rows, the parts around its gate (the second projection and the other products are
  * mb_linear_fp8_fwd and mb_linear_fp8_wgrad):
  *
- * mb_geglu_fp8_act      act = GeLU(x W1) (*) x V, fp32 up to the store in 8 bits; neither projection is written to memory.
+ * mb_geglu_fp8_act      act = GeLU(x W1) (*) x V; neither projection is written to memory.  Their sums are those of
+ *                       mb_linear_fp8_fwd for MB_BF16 (not rounded to bf16), the gate is fp32.
  *   xq, xs      dev, rows [T_cap, hidden], read.
  *   w1vq, w1vs  dev, weight [2*inter, hidden], W1 transposed over V transposed as in mb_geglu_fwd, read.
  *   actq, acts  dev, rows [T_cap, inter], written.

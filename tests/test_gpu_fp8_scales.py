@@ -187,3 +187,14 @@ def test_act_beside_one_large_channel():
     value, off = orc.gelu(h)[0], np.abs(orc.gelu(h + eps[:, :inter])[0] - orc.gelu(h)[0])
     assert h.max() < -4 and np.isfinite(val(q)).all()
     check_eight(q, s, value * g, off * (np.abs(g) + eps[:, inter:]) + np.abs(value) * eps[:, inter:] + 5e-5 * np.abs(value * g))
+
+
+def test_linear_of_cancelling_sums():
+    """What a caller gets by asking for fp32 results: sums of fp32, where the others are off by what their groups drop."""
+    x, w = cancelling()
+    (_, xq, xs), (_, wq, ws) = stored(x), stored(w, 128)
+    y, A = x @ w.T, np.abs(x) @ np.abs(w).T
+    fine = mb.mb_linear_fp8_fwd(xq, xs, wq, ws, dtype=torch.float32).double().cpu().numpy()
+    rough = mb.mb_linear_fp8_fwd(xq, xs, wq, ws).double().cpu().numpy()
+    assert np.all(np.abs(fine - y) <= 136 * 2.0 ** -24 * A)
+    assert np.all(np.abs(rough - y) <= 136 * 2.0 ** -24 * A + 7 * 2.0 ** -13 * A + 2.0 ** -8 * np.abs(y))
