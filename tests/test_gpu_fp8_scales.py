@@ -1,11 +1,12 @@
-"""Scales of the 8-bit results where they hang by a thread: sums that cancel, gates far below zero, slopes next to their zero."""
+"""Scales of the 8-bit results where they hang by a thread: sums that cancel, gates far below zero, slopes next to their zero; values that
+are not finite, and the first and the last scale byte, through the operators."""
 import numpy as np
 import pytest
 import torch
 
 from oracle import fp8_oracle as orc
 from paper_2312_17482_amd import binding as mb
-from tests.test_gpu_fp8 import BF16, bf16, check_eight, dev, exps, stored, val
+from tests.test_gpu_fp8 import BF16, E4M3, E8M0, bf16, check_eight, dev, exps, stored, val
 
 pytestmark = pytest.mark.gpu
 
@@ -198,3 +199,151 @@ def test_linear_of_cancelling_sums():
     rough = mb.mb_linear_fp8_fwd(xq, xs, wq, ws).double().cpu().numpy()
     assert np.all(np.abs(fine - y) <= 136 * 2.0 ** -24 * A)
     assert np.all(np.abs(rough - y) <= 136 * 2.0 ** -24 * A + 7 * 2.0 ** -13 * A + 2.0 ** -8 * np.abs(y))
+
+
+def test_act_of_what_is_not_finite():
+    """NaN in a token, in a weight's row, and sums beyond the largest float: stored as NaN, without a part in the scale."""
+    T, hidden, inter = 70, 256, 256
+    rng = np.random.default_rng(3)
+    x, w = rng.standard_normal((T, hidden)), rng.standard_normal((2 * inter, hidden)) * 0.1
+    x[4, 130] = np.nan                                            # the token
+    w[7, 3], w[inter + 200, 250] = np.nan, np.inf                 # columns 7 and 200
+    x[9] *= 2.0 ** 100                                            # h g some 2^200: every column of the token
+    x[10, :], x[10, 0] = 0.0, 1e-30
+    (xv, xq, xs), (wv, wq, ws) = stored(x), stored(w, 128)
+    q, s = mb.mb_geglu_fp8_act(xq, xs, wq, ws)
+    hg = xv @ wv.T
+    v = orc.gelu(hg[:, :inter])[0] * hg[:, inter:]
+    v[9] = np.where(np.abs(v[9]) > 1e38, np.inf, v[9])            # (or 0, where the gate is far below zero)
+    assert np.array_equal(np.isnan(val(q)), ~np.isfinite(v)) and np.isnan(val(q)[[4]]).all() and np.isnan(val(q)[:, [7, 200]]).all()
+    fine, e = np.isfinite(v), np.repeat(exps(s), 128, 1)
+    plain = np.ones(T, dtype=bool)
+    plain[[9]] = False
+    A = np.abs(np.where(np.isnan(xv), 0, xv)) @ np.abs(np.where(np.isnan(wv), 0, wv)).T
+    err = 2 * (7 * 2.0 ** -13 + 300 * 2.0 ** -24) * (np.abs(hg[:, inter:]) * 1.2 * A[:, :inter] + np.abs(hg[:, :inter]) * A[:, inter:]) + 2e-4 * np.abs(v)
+    off = np.abs(val(q) * np.ldexp(1.0, e) - v)
+    assert np.all((off <= 2.0 ** -4 * np.abs(v) + 2.0 ** -10 * np.ldexp(1.0, e) + err)[fine & plain[:, None]])
+    assert np.all(exps(s)[4] == -126)
+    clean = np.abs(np.where(fine, v, 0)).reshape(T, 2, 128).max(2)
+    worst = np.where(fine, err, 0).reshape(T, 2, 128).max(2)
+    most = np.ldexp(448.0, exps(s))
+    assert np.all(((clean - worst <= most) & ((clean + worst > most / 2) | (exps(s) == -126)))[plain])
+
+
+@pytest.mark.parametrize("T", [5, 300])
+def test_gate_backward_of_what_is_not_finite(T):
+    """Infinities and NaN in da, h and g are stored as NaN, and the block's scale is that of the others."""
+    inter, inf, nan = 256, np.inf, np.nan
+    rng = np.random.default_rng(4)
+    da, hg = bf16(rng.standard_normal((T, inter))), bf16(rng.standard_normal((T, 2 * inter)))
+    da[0, :3], hg[1, :3], hg[2, inter:inter + 3] = [inf, -inf, nan], [inf, -inf, nan], [inf, -inf, nan]
+    da[3, :128] = nan
+    hg[4, :4], hg[4, inter + 4] = [5e37, -5e37, 1e30, -1e30], 5e37
+    da, hg = bf16(da), bf16(hg)
+    q, s = mb.mb_gelu_gate_fp8_bwd(dev(da, BF16), dev(hg, BF16))
+    with np.errstate(all="ignore"):
+        value, slope = orc.gelu(hg[:, :inter])
+        v = np.concatenate([da * (hg[:, inter:] * slope), da * value], 1)
+    want, e = orc.store(v)
+    assert np.array_equal(exps(s), e)
+    assert np.array_equal(np.isnan(val(q)), np.isnan(want)) and np.isnan(want).sum() >= 3 * 5 + 128
+    fine = ~np.isnan(want)
+    off = np.abs(val(q) * np.ldexp(1.0, np.repeat(e, 128, 1)) - v)
+    assert np.all((off <= 2.0 ** -4 * (1 + 1e-3) * np.abs(v) + 2.0 ** -10 * np.ldexp(1.0, np.repeat(e, 128, 1)))[fine])
+
+
+# ---------------------------------------------------------------------------------------------------- every scale byte
+def coded(q, b, rows=1):
+    """8-bit rows with the given scale bytes: (values in 64 bits, q and s on the GPU)."""
+    dq = torch.from_numpy(q.astype(np.float32)).to(E4M3)
+    assert np.array_equal(val(dq), q, equal_nan=True)
+    scale = np.where(b == 255, np.nan, np.ldexp(1.0, b.astype(int) - 127))
+    values = q * np.repeat(np.repeat(scale, rows, 0), 128, 1)[:q.shape[0], :q.shape[1]]
+    return values, dq.cuda(), torch.from_numpy(b.astype(np.uint8)).view(E8M0).cuda()
+
+
+def codes_of(rng, *shape):
+    return np.ldexp(8.0 + rng.integers(0, 8, shape), rng.integers(-2, 3, shape)) * rng.choice([-1.0, 1.0], shape)
+
+
+@pytest.mark.parametrize("dtype", [BF16, torch.float32])
+@pytest.mark.parametrize("T,n_in,n_out", [(3, 384, 272), (70, 384, 784), (500, 384, 784), (2500, 384, 784), (12000, 384, 2064)])
+def test_products_under_the_first_and_the_last_scale(T, n_in, n_out, dtype):
+    """Scale byte 0 is 2^-127, 255 is NaN, also for codes that are 0; both apply to their block alone."""
+    rng = np.random.default_rng(T)
+    x, w = codes_of(rng, T, n_in), codes_of(rng, n_out, n_in)
+    xb, wb = np.full((T, 3), 127), np.full((-(-n_out // 128), 3), 127)
+    xb[1, :], wb[1, :] = 0, 247                                   # 2^-127 and 2^120: results of some 2^6
+    xb[2, 1], x[2, 128:256], wb[2, 2], w[256:272, 256:] = 255, 0.0, 255, 0.0
+    xb[0, :] = 60
+    xv, xq, xs = coded(x, xb)
+    wv, wq, ws = coded(w, wb, 128)
+    got = mb.mb_linear_fp8_fwd(xq, xs, wq, ws, dtype=dtype).double().cpu().numpy()
+    y, A = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    beyond = A > 1e38                                             # (row blocks under 2^127 with ordinary ones)
+    nan = np.isnan(y)
+    assert nan.any() and np.array_equal(np.isnan(got) & ~beyond, nan)
+    fine = ~nan & ~beyond
+    fast = dtype == BF16
+    assert fine[1, 128:256].all()
+    assert np.all(np.abs(got - y)[fine] <= ((n_in + 8) * 2.0 ** -24 * A + (7 * 2.0 ** -13 * A + 2.0 ** -8 * np.abs(y) if fast else 0) + 1e-37)[fine])
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("T,n_in,n_out", [(5, 144, 80), (300, 1040, 400), (6000, 784, 528), (12000, 528, 528)])
+def test_weight_gradient_under_the_first_and_the_last_scale(T, n_in, n_out, eight):
+    rng = np.random.default_rng(T)
+    x, xb = codes_of(rng, T, n_in), np.full((T, -(-n_in // 128)), 127)
+    xb[1, 1], x[1, 128:], xb[0, 0] = 255, 0.0, 0
+    xv, xq, xs = coded(x, xb)
+    if eight:
+        dyb = np.full((T, -(-n_out // 128)), 127)
+        dyb[0, :] = 254 - 20
+        dyv, dyq, dys = coded(codes_of(rng, T, n_out), dyb)
+    else:
+        dyv = bf16(rng.standard_normal((T, n_out)))
+        dyv[0] *= 2.0 ** 107
+        dyq, dys = dev(dyv, BF16), None
+    xv[0, 128:] = 0.0
+    xq.view(torch.uint8)[0, 128:] = 0
+    got = mb.mb_linear_fp8_wgrad(dyq, xq, xs, dys=dys).double().cpu().numpy()
+    want, A = dyv.T @ xv, np.abs(dyv).T @ np.abs(xv)
+    nan = np.isnan(want)
+    assert np.array_equal(np.isnan(got), nan) and nan[:, 128:min(256, n_in)].all() and not nan[:, :128].any()
+    assert np.all(np.abs(got - want)[~nan] <= ((T + 40) * 2.0 ** -24 * A + 1e-37)[~nan])
+
+
+def test_gate_under_the_first_and_the_last_scale():
+    T, hidden, inter = 70, 256, 256
+    rng = np.random.default_rng(8)
+    x, w = codes_of(rng, T, hidden), codes_of(rng, 2 * inter, hidden)
+    xb, wb = np.full((T, 2), 120), np.full((4, 2), 119)
+    xb[1, 0], x[1, :128], wb[1, 1] = 255, 0.0, 255                # token 1; h of columns 128 ..
+    xb[2, :], wb[0, :], wb[2, :] = 0, 240, 240
+    x[3:] = 0.0
+    x[0] = 0.0
+    xv, xq, xs = coded(x, xb)
+    wv, wq, ws = coded(w, wb, 128)
+    q, s = mb.mb_geglu_fp8_act(xq, xs, wq, ws)
+    hg, A = xv @ wv.T, np.abs(xv) @ np.abs(wv).T
+    v = orc.gelu(hg[:, :inter])[0] * hg[:, inter:]
+    assert np.array_equal(np.isnan(val(q)), np.isnan(v)) and np.isnan(v[1]).all() and np.isnan(v[:, 128:]).all() and np.isfinite(v[2, :128]).all()
+    err = 2 * (7 * 2.0 ** -13 + 300 * 2.0 ** -24) * (np.abs(hg[:, inter:]) * 1.2 * A[:, :inter] + np.abs(hg[:, :inter]) * A[:, inter:]) + 2e-4 * np.abs(v)
+    sc, fine = np.repeat(np.ldexp(1.0, exps(s)), 128, 1), np.isfinite(v)
+    assert np.all((np.abs(val(q) * sc - v) <= 2.0 ** -4 * np.abs(v) + 2.0 ** -10 * sc + err)[fine])
+    assert np.all(exps(s)[1] == -126) and np.all(exps(s)[:, 1] == -126)
+    # backward: h | g in 8 bits
+    hq, hb = codes_of(rng, T, 2 * inter), np.full((T, 4), 122)
+    hb[1, 0], hq[1, :128], hb[2, 2], hb[4, 1] = 255, 0.0, 0, 255
+    hv, hgq, hgs = coded(hq, hb)
+    da = bf16(rng.standard_normal((T, inter)))
+    da[2, :128] *= 2.0 ** 60
+    da = bf16(da)
+    q, s = mb.mb_gelu_gate_fp8_bwd(dev(da, BF16), hgq, hgs)
+    value, slope = orc.gelu(hv[:, :inter])
+    v = np.concatenate([da * (hv[:, inter:] * slope), da * value], 1)
+    want, e = orc.store(v)
+    assert np.array_equal(np.isnan(val(q)), np.isnan(want)) and np.isnan(want).sum() == 4 * 128
+    assert np.array_equal(exps(s), e)
+    sc, fine = np.repeat(np.ldexp(1.0, e), 128, 1), ~np.isnan(want)
+    assert np.all((np.abs(val(q) * sc - v) <= 2.0 ** -4 * (1 + 1e-3) * np.abs(v) + 2.0 ** -10 * sc)[fine])
