@@ -347,3 +347,28 @@ def test_gate_under_the_first_and_the_last_scale():
     assert np.array_equal(exps(s), e)
     sc, fine = np.repeat(np.ldexp(1.0, e), 128, 1), ~np.isnan(want)
     assert np.all((np.abs(val(q) * sc - v) <= 2.0 ** -4 * (1 + 1e-3) * np.abs(v) + 2.0 ** -10 * sc)[fine])
+
+
+@pytest.mark.parametrize("eight", [False, True])
+def test_gate_backward_decides_beside_a_border_in_64_bits(eight):
+    """Blocks of one gradient each, da g GeLU'(h) within 1e-5 of 448 * 2^e: less than what 32 bits leave of many of them."""
+    bits = 3 if eight else 7
+    m = 1.0 + np.arange(2 ** bits) / 2.0 ** bits
+    h = np.concatenate([-np.ldexp(m, k) for k in range(4)] + [np.ldexp(m, k) for k in (-1, 0)])
+    h, a, g = (x.ravel() for x in np.meshgrid(h[h > -11], 1.0 + np.arange(128) / 128.0, m, indexing="ij"))
+    v = np.abs(a * g * orc.gelu(h)[1])
+    off = np.abs(v / np.ldexp(448.0, np.floor(np.log2(v / 448.0) + 0.5).astype(int)) - 1)
+    pick = np.flatnonzero((off < (1e-4 if eight else 1e-5)) & (off > 1e-8))
+    assert len(pick) >= (4 if eight else 100)
+    da, hg = np.zeros((len(pick), 128)), np.zeros((len(pick), 256))
+    at = np.arange(len(pick)) % 128                                # (by every lane and place in it)
+    da[np.arange(len(pick)), at], hg[np.arange(len(pick)), at], hg[np.arange(len(pick)), 128 + at] = a[pick], h[pick], g[pick]
+    if eight:
+        hg, hgq, hgs = stored(hg)
+    else:
+        hgq, hgs = dev(hg, BF16), None
+    _, s = mb.mb_gelu_gate_fp8_bwd(dev(da, BF16), hgq, hgs)
+    value, slope = orc.gelu(hg[:, :128])
+    want = orc.scale_exponents(np.concatenate([da * hg[:, 128:] * slope, da * value], 1))
+    print(len(pick), "blocks,", (exps(s) != want).sum(0), "scales not the definition's")
+    assert np.array_equal(exps(s)[:, 0], want[:, 0])
