@@ -546,8 +546,15 @@ int rows_used(const Args<N>& a, int i, int64_t rows) {
   require(T_cap <= rows, "T_cap is more rows than there are");
   return T_cap;
 }
+// The row count on the device.  (A tensor; of an object that only has a pointer nothing more is known.)
 template <int N>
-const int32_t* meta_of(const Args<N>& a, int i) { return (const int32_t*)a.ptr(i); }
+const int32_t* meta_of(const Args<N>& a, int i, const at::Tensor& like) {
+  if (a.given(i) && THPVariable_Check(a.v[i])) {
+    const at::Tensor& m = a.tensor(i);
+    require(m.scalar_type() == at::kInt && m.numel() > 0 && m.device() == like.device(), "meta must be int32, on the tensors' device");
+  }
+  return (const int32_t*)a.ptr(i);
+}
 
 PyObject* quant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   static const Names names("x", "T_cap", "meta", "q", "s");
@@ -561,7 +568,7 @@ PyObject* quant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   stored(q.tensor(a, 3), sc.tensor(a, 4));
   require(q.tensor(a, 3).size(0) >= T_cap && q.tensor(a, 3).size(1) == W, "q must have x's columns and as many rows as are used");
   together(s, x, q.tensor(a, 3), sc.tensor(a, 4));
-  run(s, s->quant, (const void*)x.data_ptr(), stride, T_cap, meta_of(a, 2), (int)W, dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+  run(s, s->quant, (const void*)x.data_ptr(), stride, T_cap, meta_of(a, 2, x), (int)W, dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
       current_stream(s));
   return tuple_of(q.take(), sc.take());
 }
@@ -587,7 +594,7 @@ PyObject* dequant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(o.size(0) >= T_cap && o.size(1) == W, "out must have q's columns and as many rows as are used");
   require(!a.given(2) || o.scalar_type() == type_or_bf16(a, 2), "out is of another dtype");
   together(s, q, sc, o);
-  run(s, s->dequant, (const uint8_t*)q.data_ptr(), (const uint8_t*)sc.data_ptr(), T_cap, meta_of(a, 4), (int)W,
+  run(s, s->dequant, (const uint8_t*)q.data_ptr(), (const uint8_t*)sc.data_ptr(), T_cap, meta_of(a, 4, q), (int)W,
       (mb_dtype)dtype_code(o), out.ptr, stride, current_stream(s));
   return out.take();
 }
@@ -634,7 +641,7 @@ PyObject* linear(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(!a.given(4) || o.scalar_type() == type_or_bf16(a, 4), "y is of another dtype");
   together(s, xq, xs, wq, ws, o);
   run(s, s->linear, (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), (const uint8_t*)wq.data_ptr(),
-      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 6), (int)n_in, (int)n_out, (mb_dtype)dtype_code(o), y.ptr, stride,
+      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 6, xq), (int)n_in, (int)n_out, (mb_dtype)dtype_code(o), y.ptr, stride,
       current_stream(s));
   return y.take();
 }
@@ -656,10 +663,12 @@ PyObject* wgrad(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
           "dw must be a contiguous float32 matrix [columns of dy, columns of x]");
   const size_t need = a.given(7) ? 0 : s->wgrad_bytes(T_cap, (int)n_in, (int)n_out);
   Result workspace(a, 7, [&] { return new_bytes(xq, need); });
+  if (a.given(7) && THPVariable_Check(a.v[7]))
+    require(a.tensor(7).device() == xq.device() && a.tensor(7).is_contiguous(), "workspace must be contiguous, on the tensors' device");
   if (eight) together(s, dy, a.tensor(3), xq, xs, o);
   else together(s, dy, xq, xs, o);
   run(s, s->wgrad, (const void*)dy.data_ptr(), eight ? (const uint8_t*)a.ptr(3) : nullptr, eight ? n_out : stride,
-      (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), T_cap, meta_of(a, 5), (int)n_in, (int)n_out, (float*)dw.ptr,
+      (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), T_cap, meta_of(a, 5, xq), (int)n_in, (int)n_out, (float*)dw.ptr,
       workspace.ptr, workspace.numel(a, 7), current_stream(s));
   return dw.take();
 }
@@ -679,7 +688,7 @@ PyObject* geglu_act(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(q.tensor(a, 6).size(0) >= T_cap && q.tensor(a, 6).size(1) == inter, "actq must have inter columns and as many rows as are used");
   together(s, xq, xs, wq, ws, q.tensor(a, 6), sc.tensor(a, 7));
   run(s, s->act, (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), (const uint8_t*)wq.data_ptr(),
-      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 5), (int)hidden, (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 5, xq), (int)hidden, (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
       current_stream(s));
   return tuple_of(q.take(), sc.take());
 }
@@ -702,7 +711,7 @@ PyObject* gate_bwd(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   if (eight) together(s, da, hg, a.tensor(2), q.tensor(a, 5), sc.tensor(a, 6));
   else together(s, da, hg, q.tensor(a, 5), sc.tensor(a, 6));
   run(s, s->gate_bwd, (const void*)da.data_ptr(), (const void*)hg.data_ptr(), eight ? (const uint8_t*)a.ptr(2) : nullptr, T_cap,
-      meta_of(a, 4), (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr, current_stream(s));
+      meta_of(a, 4, da), (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr, current_stream(s));
   return tuple_of(q.take(), sc.take());
 }
 
