@@ -14,6 +14,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
 
+#include <algorithm>
+#include <climits>
 #include <cstdint>
 #include <functional>
 #include <utility>
@@ -540,11 +542,18 @@ int64_t matrix_stride(const at::Tensor& t) {
   require(t.dim() == 2 && (t.stride(1) == 1 || t.size(1) <= 1), "need a matrix with dense rows");
   return t.size(0) > 1 ? t.stride(0) : std::max(t.stride(0), t.size(1));
 }
+// A size as the library takes it: one that is no int is too large for it in any case.
+int size_of(int64_t n) { return (int)std::clamp<int64_t>(n, INT_MIN, INT_MAX); }
 template <int N>
 int rows_used(const Args<N>& a, int i, int64_t rows) {
-  const int T_cap = a.integer_or(i, rows);
+  if (!a.given(i)) return size_of(rows);
+  PyObject* x = PyNumber_Index(a.v[i]);
+  if (!x) throw Raised();
+  const long long T_cap = PyLong_AsLongLong(x);
+  Py_DECREF(x);
+  if (T_cap == -1 && PyErr_Occurred()) throw Raised();
   require(T_cap <= rows, "T_cap is more rows than there are");
-  return T_cap;
+  return size_of(T_cap);
 }
 // The row count on the device.  (A tensor; of an object that only has a pointer nothing more is known.)
 template <int N>
@@ -568,7 +577,7 @@ PyObject* quant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   stored(q.tensor(a, 3), sc.tensor(a, 4));
   require(q.tensor(a, 3).size(0) >= T_cap && q.tensor(a, 3).size(1) == W, "q must have x's columns and as many rows as are used");
   together(s, x, q.tensor(a, 3), sc.tensor(a, 4));
-  run(s, s->quant, (const void*)x.data_ptr(), stride, T_cap, meta_of(a, 2, x), (int)W, dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+  run(s, s->quant, (const void*)x.data_ptr(), stride, T_cap, meta_of(a, 2, x), size_of(W), dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
       current_stream(s));
   return tuple_of(q.take(), sc.take());
 }
@@ -594,7 +603,7 @@ PyObject* dequant(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(o.size(0) >= T_cap && o.size(1) == W, "out must have q's columns and as many rows as are used");
   require(!a.given(2) || o.scalar_type() == type_or_bf16(a, 2), "out is of another dtype");
   together(s, q, sc, o);
-  run(s, s->dequant, (const uint8_t*)q.data_ptr(), (const uint8_t*)sc.data_ptr(), T_cap, meta_of(a, 4, q), (int)W,
+  run(s, s->dequant, (const uint8_t*)q.data_ptr(), (const uint8_t*)sc.data_ptr(), T_cap, meta_of(a, 4, q), size_of(W),
       (mb_dtype)dtype_code(o), out.ptr, stride, current_stream(s));
   return out.take();
 }
@@ -619,7 +628,7 @@ PyObject* quant_weight(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(q.tensor(a, 2).sizes() == w.sizes(), "q must have w's shape");
   require(!both || (qt.tensor(a, 4).size(0) == n_in && qt.tensor(a, 4).size(1) == n_out), "qt must have w's shape transposed");
   together(s, w, q.tensor(a, 2), sc.tensor(a, 3), qt.tensor(a, 4), st.tensor(a, 5));
-  run(s, s->quant_weight, (const void*)w.data_ptr(), (int)n_out, (int)n_in, dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+  run(s, s->quant_weight, (const void*)w.data_ptr(), size_of(n_out), size_of(n_in), dt, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
       both ? (uint8_t*)qt.ptr : nullptr, both ? (uint8_t*)st.ptr : nullptr, current_stream(s));
   if (!both) return tuple_of(q.take(), sc.take());
   return tuple_of(q.take(), sc.take(), qt.take(), st.take());
@@ -641,7 +650,7 @@ PyObject* linear(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(!a.given(4) || o.scalar_type() == type_or_bf16(a, 4), "y is of another dtype");
   together(s, xq, xs, wq, ws, o);
   run(s, s->linear, (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), (const uint8_t*)wq.data_ptr(),
-      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 6, xq), (int)n_in, (int)n_out, (mb_dtype)dtype_code(o), y.ptr, stride,
+      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 6, xq), size_of(n_in), size_of(n_out), (mb_dtype)dtype_code(o), y.ptr, stride,
       current_stream(s));
   return y.take();
 }
@@ -661,14 +670,14 @@ PyObject* wgrad(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   const at::Tensor& o = dw.tensor(a, 6);
   require(o.scalar_type() == at::kFloat && o.dim() == 2 && o.is_contiguous() && o.size(0) == n_out && o.size(1) == n_in,
           "dw must be a contiguous float32 matrix [columns of dy, columns of x]");
-  const size_t need = a.given(7) ? 0 : s->wgrad_bytes(T_cap, (int)n_in, (int)n_out);
+  const size_t need = a.given(7) ? 0 : s->wgrad_bytes(T_cap, size_of(n_in), size_of(n_out));
   Result workspace(a, 7, [&] { return new_bytes(xq, need); });
   if (a.given(7) && THPVariable_Check(a.v[7]))
     require(a.tensor(7).device() == xq.device() && a.tensor(7).is_contiguous(), "workspace must be contiguous, on the tensors' device");
   if (eight) together(s, dy, a.tensor(3), xq, xs, o);
   else together(s, dy, xq, xs, o);
   run(s, s->wgrad, (const void*)dy.data_ptr(), eight ? (const uint8_t*)a.ptr(3) : nullptr, eight ? n_out : stride,
-      (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), T_cap, meta_of(a, 5, xq), (int)n_in, (int)n_out, (float*)dw.ptr,
+      (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), T_cap, meta_of(a, 5, xq), size_of(n_in), size_of(n_out), (float*)dw.ptr,
       workspace.ptr, workspace.numel(a, 7), current_stream(s));
   return dw.take();
 }
@@ -688,7 +697,7 @@ PyObject* geglu_act(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   require(q.tensor(a, 6).size(0) >= T_cap && q.tensor(a, 6).size(1) == inter, "actq must have inter columns and as many rows as are used");
   together(s, xq, xs, wq, ws, q.tensor(a, 6), sc.tensor(a, 7));
   run(s, s->act, (const uint8_t*)xq.data_ptr(), (const uint8_t*)xs.data_ptr(), (const uint8_t*)wq.data_ptr(),
-      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 5, xq), (int)hidden, (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
+      (const uint8_t*)ws.data_ptr(), T_cap, meta_of(a, 5, xq), size_of(hidden), size_of(inter), (uint8_t*)q.ptr, (uint8_t*)sc.ptr,
       current_stream(s));
   return tuple_of(q.take(), sc.take());
 }
@@ -711,7 +720,7 @@ PyObject* gate_bwd(Self8 s, Argv argv, Py_ssize_t n, PyObject* kw) {
   if (eight) together(s, da, hg, a.tensor(2), q.tensor(a, 5), sc.tensor(a, 6));
   else together(s, da, hg, q.tensor(a, 5), sc.tensor(a, 6));
   run(s, s->gate_bwd, (const void*)da.data_ptr(), (const void*)hg.data_ptr(), eight ? (const uint8_t*)a.ptr(2) : nullptr, T_cap,
-      meta_of(a, 4, da), (int)inter, (uint8_t*)q.ptr, (uint8_t*)sc.ptr, current_stream(s));
+      meta_of(a, 4, da), size_of(inter), (uint8_t*)q.ptr, (uint8_t*)sc.ptr, current_stream(s));
   return tuple_of(q.take(), sc.take());
 }
 

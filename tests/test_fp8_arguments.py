@@ -27,3 +27,39 @@ def test_a_workspace_that_the_kernels_cannot_use(recorded):
         with pytest.raises(AssertionError):
             calls.mb_linear_fp8_wgrad(**calls_with("mb_linear_fp8_wgrad", workspace=work))
     assert "mb_linear_fp8_wgrad" not in seen
+
+
+def test_sizes_of_more_than_32_bits_do_not_wrap(recorded):
+    """They arrive as the largest int, which the library refuses; modulo 2^32 they would be small sizes that look right."""
+    calls, seen = recorded
+    most, far = 2 ** 31 - 1, 2 ** 32 + 16
+
+    def rows(n, width, dtype=E4M3, block=1):
+        q = torch.empty((n, width), dtype=dtype, device="meta")
+        return q, torch.empty((-(-n // block), -(-width // 128)), dtype=E8M0, device="meta")
+
+    calls.mb_fp8_quant(rows(far, 16, torch.bfloat16)[0])
+    assert seen["mb_fp8_quant"]["T_cap"] == most
+    calls.mb_fp8_dequant(*rows(far, 16))
+    assert seen["mb_fp8_dequant"]["T_cap"] == most
+    calls.mb_fp8_dequant(*rows(1, far))
+    assert seen["mb_fp8_dequant"]["W"] == most
+    calls.mb_fp8_quant_weight(rows(far, 16, torch.bfloat16)[0])
+    assert seen["mb_fp8_quant_weight"]["n_out"] == most and seen["mb_fp8_quant_weight"]["n_in"] == 16
+    calls.mb_linear_fp8_fwd(*rows(1, far), *rows(16, far, block=128))
+    assert seen["mb_linear_fp8_fwd"]["n_in"] == most
+    calls.mb_linear_fp8_wgrad(rows(far, 16, torch.bfloat16)[0], *rows(far, 16))
+    assert seen["mb_linear_fp8_wgrad"]["T_cap"] == most
+    calls.mb_geglu_fp8_act(*rows(far, 16), *rows(256, 16, block=128))
+    assert seen["mb_geglu_fp8_act"]["T_cap"] == most
+    calls.mb_gelu_gate_fp8_bwd(rows(far, 128, torch.bfloat16)[0], rows(far, 256, torch.bfloat16)[0])
+    assert seen["mb_gelu_gate_fp8_bwd"]["T_cap"] == most
+    seen.clear()
+    x = torch.zeros(20, 144)
+    for count in (2 ** 32 + 5, 21):
+        with pytest.raises(AssertionError):
+            calls.mb_fp8_quant(x, T_cap=count)
+    calls.mb_fp8_quant(rows(far, 16, torch.bfloat16)[0], T_cap=5)                # few rows of many: as before
+    assert seen["mb_fp8_quant"]["T_cap"] == 5
+    calls.mb_fp8_quant(x, T_cap=-1)                                              # (the library refuses it)
+    assert seen["mb_fp8_quant"]["T_cap"] == -1
