@@ -115,8 +115,9 @@ __global__ __launch_bounds__(512, 2) void fp8_wgrad_kernel(Wgrad pr) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, g = lane >> 5;
   const int wm = wave >> 2, wn = wave & 3;
-  Stager<kEight, kM> ps(pr.dy, pr.dys, pr.dy_stride, m0, pr.n_out, T, tid);
-  Stager<true, 256> qs(pr.x, pr.xs, pr.n_in, n0, pr.n_in, T, tid);
+  const int end = min(T, (begin + nsteps) * kRows);   // (of the split's own tokens)
+  Stager<kEight, kM> ps(pr.dy, pr.dys, pr.dy_stride, m0, pr.n_out, end, tid);
+  Stager<true, 256> qs(pr.x, pr.xs, pr.n_in, n0, pr.n_in, end, tid);
 
   // Fragment reads: lane -> row tr_row (+ 8) and 4 columns of a 16 x 32 patch; P columns 32 (kMB wm + mb), Q columns
   // 64 wn + 32 nb.
