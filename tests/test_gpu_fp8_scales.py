@@ -372,3 +372,13 @@ def test_gate_backward_decides_beside_a_border_in_64_bits(eight):
     want = orc.scale_exponents(np.concatenate([da * hg[:, 128:] * slope, da * value], 1))
     print(len(pick), "blocks,", (exps(s) != want).sum(0), "scales not the definition's")
     assert np.array_equal(exps(s)[:, 0], want[:, 0])
+
+
+def test_act_of_sums_computed_too_small():
+    """The other way round: h = 3 * 2^-8 is computed as some 2^-8.  What 64 bits find beyond the border takes a scale that holds it."""
+    x, w = cancelling()
+    w[:128, 8] = -0.02734375
+    v, q, e, _, _ = act(x, w)
+    ratio = q * np.repeat(np.ldexp(1.0, e), 128, 1) / v
+    assert np.isfinite(q).all() and np.all((ratio >= (1 - 2.0 ** -4) / 3.1) & (ratio <= 1 + 2.0 ** -4))
+    assert np.all(e <= orc.scale_exponents(v))
