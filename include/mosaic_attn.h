@@ -431,7 +431,7 @@ MB_API mb_status mb_linear_fp8_wgrad(const void* dy, const uint8_t* dys, int64_t
  * Scales: a block's scale is taken from the values that are stored, so that it holds every finite one.  Where the largest lies within
  * 2.8e-4 (mb_geglu_fp8_act) or 7e-5 (mb_gelu_gate_fp8_bwd) of 448 * 2^e, the values that decide are computed again in 64 bits (and
  * stored as such by mb_geglu_fp8_act).  Scales are therefore those of the exact values wherever the computed ones are that near to
- * them.  The gate's backward is, 3.3e-5 at most; the activation is, with 1.4e-5 to 4.4e-5, unless its sums cancel or one product
+ * them.  The gate's backward is, 5.9e-5 at most; the activation is, with 1.4e-5 to 4.4e-5, unless its sums cancel or one product
  * of a group is far larger than the result: then a scale can be a neighbour of the exact values', as the value itself is off.
  * Time: a tenth of mb_geglu_fp8_act, a fifth for some hundred tokens; a batch made of little else (every column of every token just
  * below a border) takes some hundred times as long.

@@ -168,9 +168,9 @@ __global__ __launch_bounds__(256) void fp8_quant_weight_kernel(const T* __restri
 __device__ __forceinline__ double bf16_value(uint16_t b) { return (double)__uint_as_float((uint32_t)b << 16); }
 
 // Backward of the gate act = GeLU(h) (*) g from dA and h | g (bf16, or 8 bits with scales): dh | dg in 8 bits.  Eight lanes
-// per 128 columns, 16 values of dA, h and g each; both results' blocks are those lanes' own.  (26963 x 3072, h | g in 8 bits: 98 to 101 us,
-// 5.0 TB/s; two transcendentals and some 30 other instructions a value stay under the memory's time.)
-constexpr uint32_t kReach = 1024;   // 7e-5 of a value, twice what gelu_tail_and_grad leaves
+// per 128 columns, 16 values of dA, h and g each; both results' blocks are those lanes' own.  (26963 x 3072, h | g in 8 bits: 98 us,
+// 5.1 TB/s; two transcendentals and some 30 other instructions a value stay just under the memory's time.)
+constexpr uint32_t kReach = 1024;   // 7e-5 of a value; gelu_tail_and_grad leaves 5.9e-5 beside the derivative's zero and 9e-6 elsewhere
 template <bool kEight>
 __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __restrict__ da, const void* __restrict__ hg,
                                                            const uint8_t* __restrict__ hgs, int T_cap,
@@ -214,7 +214,7 @@ __global__ __launch_bounds__(256) void fp8_gate_bwd_kernel(const uint16_t* __res
     gelu_tail_and_grad(h[i], val, grad);
     h[i] = a[i] * (g[i] * grad);   // (a g may be beyond the largest float where the derivative is next to nothing)
     g[i] = a[i] * val;
-    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (four values at a time: with all 16 interleaved 115 us instead of 104)
+    if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (four values at a time: 98 us, with all 16 interleaved 107)
   }
   float htop = max_of_8_lanes(largest_of_16(h)), gtop = max_of_8_lanes(largest_of_16(g));
   if (__builtin_expect(__ballot(near_border(htop, kReach) || near_border(gtop, kReach)) != 0, 0)) {

@@ -382,3 +382,21 @@ def test_act_of_sums_computed_too_small():
     ratio = q * np.repeat(np.ldexp(1.0, e), 128, 1) / v
     assert np.isfinite(q).all() and np.all((ratio >= (1 - 2.0 ** -4) / 3.1) & (ratio <= 1 + 2.0 ** -4))
     assert np.all(e <= orc.scale_exponents(v))
+
+
+def test_gate_backward_decides_beside_the_slopes_zero():
+    """Every bf16 h within 0.04 of it, da g GeLU'(h) within 1e-4 of 448 * 2^e."""
+    h = -np.arange(0.7109375, 0.79296875, 2.0 ** -8)               # (the step of bf16 there)
+    m = 1.0 + np.arange(128) / 128.0
+    h, a, g = (x.ravel() for x in np.meshgrid(h, m, m, indexing="ij"))
+    slope = orc.gelu(h)[1]
+    v = np.abs(a * g * slope)
+    off = np.abs(v / np.ldexp(448.0, np.floor(np.log2(v / 448.0) + 0.5).astype(int)) - 1)
+    pick = np.flatnonzero((off < 1e-4) & (off > 1e-8 + 4e-10 * 0.5 / np.abs(slope)))
+    assert len(pick) > 50 and len(np.unique(h[pick])) > 15
+    da, hg = np.zeros((len(pick), 128)), np.zeros((len(pick), 256))
+    at = np.arange(len(pick)) % 128
+    da[np.arange(len(pick)), at], hg[np.arange(len(pick)), at], hg[np.arange(len(pick)), 128 + at] = a[pick], h[pick], g[pick]
+    assert np.array_equal(bf16(hg), hg)
+    _, s = mb.mb_gelu_gate_fp8_bwd(dev(da, BF16), dev(hg, BF16))
+    assert np.array_equal(exps(s)[:, 0], orc.scale_exponents((da * hg[:, 128:] * orc.gelu(hg[:, :128])[1]))[:, 0])
