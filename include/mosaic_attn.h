@@ -360,7 +360,8 @@ MB_API mb_status mb_gelu_gate(const void* h, const void* gate, int64_t row_strid
  * infinity) times a scale 2^(b - 127), whose byte b (E8M0, 255 = NaN) serves
  *   rows     128 values of a row: q [T, W], s [T, ceil(W / 128)], the last block of a row may be shorter;
  *   weights  a 128 x 128 block: q [n_out, n_in], s [ceil(n_out / 128), ceil(n_in / 128)], blocks at the ends may be smaller.
- * All four are contiguous.  Widths are multiples of 16 up to 2^20.  Powers of two round nothing: x = q 2^(b - 127) is exact in
+ * All four are contiguous and, scales too, 16-byte aligned (so that rows from the i-th on can be a call's own where
+ * i * ceil(W / 128) is a multiple of 16).  Widths are multiples of 16 up to 2^20.  Powers of two round nothing: x = q 2^(b - 127) is exact in
  * float and, where it is a normal number, in bfloat16 (the largest floats, over 248 * 2^120, round up to 2^128: infinite again
  * as a float).
  *   Storing a block takes the smallest scale 2^e, e >= -126, with every finite |x| <= 448 * 2^e, and rounds x / 2^e to the nearest
